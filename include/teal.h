@@ -423,6 +423,142 @@ teal_status teal_sparse_gemv_w4_multi(int count, const uint8_t *const *Wq,
                                       void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Microscaled 4-bit weights (mx4): 32 neighbouring outputs of one input channel are
+ * a block, which shares a power of two X; a weight is X times one of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and a sign (the E2M1 numbers and E8M0 scales of microscaled formats).
+ * The blocks lie along the outputs and not along the sum: input sparsity keeps or
+ * drops a channel, and a dropped channel takes its scales with it.
+ *   Wq    [m][n/2] bytes, two codes per byte along the output axis, low nibble =
+ *         even j; code = sign << 3 | index of the level above; 16-byte aligned.
+ *   scale teal_mx4_scale_bytes(m, n) bytes, 16-byte aligned: the byte 127 + log2 X
+ *         of channel i and block b = j / 32 is at
+ *             ((i / 8) * ceil(n / 512) + b / 16) * 128 + (i % 8) * 16 + b % 16,
+ *         tiles of 8 channels by 16 blocks, a cache line each.  255 makes every
+ *         weight of the block NaN.  Bytes that belong to no channel or block are
+ *         written as zeros by teal_pack_mx4 and never used.
+ *   1 <= m <= 2^24, 32 <= n <= 2^24, n % 32 == 0.
+ *
+ * teal_mx4_scale_bytes: 0 if m or n is out of range.
+ *
+ * teal_pack_mx4: canonical row-major W[n][m] bf16 -> Wq, scale (the layout step of
+ * teal_pack_bf16 with the quantisation in it).  X = 2^(floor(log2 a) - 2), a the
+ * largest magnitude of the block (never below 2^-127; a block of zeros has the
+ * byte 0), so that the largest weight lies in [4, 8) X; a weight goes to the
+ * nearest level, ties to the even code, beyond 6 X to 6 X, with its sign.  A block
+ * with a NaN or an infinity gets the byte 255.
+ * teal_unpack_mx4: the weights that Wq and scale stand for, W[n][m] bf16
+ * (exact; beyond the range of bf16, scale bytes 253 and 254, infinities).
+ * Both: device to device, out of place, W 2-byte aligned.
+ *
+ * teal_sparse_gemv_mx4: y = s_t(x) W^T, arguments as for teal_sparse_gemv_bf16 with
+ * Wq, scale in place of Wt_bf16; _multi, _swiglu and _rmsnorm_multi as the calls of
+ * these names for the other formats (count 1..4; results of _swiglu and
+ * _rmsnorm_multi are bitwise those of the producer call followed by
+ * teal_sparse_gemv_mx4 or _multi).  Scale bytes of 253 and 254 are not supported (an
+ * infinite weight may make its column NaN), weights below 2^-126 may count as zero.
+ */
+size_t teal_mx4_scale_bytes(int m, int n);
+teal_status teal_pack_mx4(const void *W_rowmajor, uint8_t *Wq, uint8_t *scale, int m, int n,
+                          void *stream);
+teal_status teal_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W_rowmajor, int m, int n,
+                            void *stream);
+teal_status teal_sparse_gemv_mx4(const uint8_t *Wq, const uint8_t *scale, const void *x_f16, float t,
+                                 float *y, int m, int n, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+teal_status teal_sparse_gemv_mx4_multi(int count, const uint8_t *const *Wq,
+                                       const uint8_t *const *scale, const float *t, float *const *y,
+                                       const int *n, const void *x_f16, int m, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+teal_status teal_sparse_gemv_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *gate,
+                                        const float *up, float t, float *y, int m, int n,
+                                        void *workspace, size_t workspace_bytes, void *stream);
+teal_status teal_sparse_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *Wq,
+                                               const uint8_t *const *scale, const float *t,
+                                               float *const *y, const int *n, const float *h,
+                                               const float *gamma, float eps, int m, void *workspace,
+                                               size_t workspace_bytes, void *stream);
+
+/*
+ * A mixture of experts: a router's choice, and the thresholded products of the
+ * experts it chose.
+ *
+ * teal_route_experts: top_k of `experts` experts and their weights, for each token.
+ *   logits [tokens][experts] fp32; bias [experts] fp32 or NULL.
+ *   score  TEAL_SCORE_SOFTMAX: s_e = exp(l_e) / sum exp(l); TEAL_SCORE_SIGMOID:
+ *          s_e = 1 / (1 + exp(-l_e)).
+ *   What experts are ranked by is v_e = s_e + bias_e, and without a bias the logit
+ *   itself (the scores increase with it).  groups > 1: the experts are that many
+ *   equal groups of neighbours, a group's value is its largest v (group_top = 1) or
+ *   the sum of its two largest s + bias (group_top = 2), and only the top_groups
+ *   groups of the largest values take part.  Of equal values the lower number comes
+ *   first, with groups and with experts.
+ *   idx    [tokens][top_k] int32: the chosen experts, the largest v first.
+ *   weight [tokens][top_k] fp32: s_e (without the bias), divided by the sum of the
+ *          token's weights if renormalise != 0 (0 if that is 0), times scaling.
+ *   Scores, v and sums are binary64; a weight is rounded once.  A NaN logit counts
+ *   as -infinity, a logit of -infinity has the score 0, one of +infinity counts as
+ *   the largest finite number; a v that is NaN comes last.
+ *   0 <= tokens <= 2^24, 1 <= experts <= TEAL_MAX_EXPERTS (else TEAL_ERR_SHAPE);
+ *   groups 1..64 divides experts, 1 <= top_groups <= groups, group_top 1 or 2,
+ *   1 <= top_k <= TEAL_MAX_TOP_K and at most the experts of top_groups groups (else
+ *   TEAL_ERR_UNSUPPORTED); scaling finite (else TEAL_ERR_THRESHOLD).
+ *
+ * teal_sparse_experts_{bf16,mx4}: y_k[b][j] = s_{t_k[e]}(x_b) W_k[e]^T with
+ * e = idx[b][j], for count (1..4) matrices per expert that read the same state: gate
+ * and up.  Every (token, expert) pair is a product of its own, with its own survivors
+ * and its expert's own threshold, in one launch.
+ *   Wt_bf16, Wq, scale, t, y, n  HOST arrays of length count.  Wt_bf16[k]: the
+ *          experts' matrices one behind the other, [experts][m][n_k] bf16, 16-byte
+ *          aligned; Wq[k] [experts][m][n_k/2], scale[k] [experts] times
+ *          teal_mx4_scale_bytes(m, n_k) bytes.  t[k]: DEVICE fp32 [experts]; it cannot
+ *          be checked, and a negative or NaN threshold counts as 0.
+ *          y[k]: [tokens][top_k][n_k] fp32.
+ *   idx    DEVICE int32 [tokens][top_k].  A number outside [0, experts) is no
+ *          expert (a padded token): zeros.  The same expert may occur again.
+ *   X_f16  [tokens][m] fp16, 2-byte aligned.
+ *   1 <= m <= 2^24, 1 <= tokens <= TEAL_MAX_BATCH, top_k up to TEAL_MAX_TOP_K, experts up
+ *   to TEAL_MAX_EXPERTS, n_k a multiple of 8 (bf16) or 32 (mx4), the sum of n_k times
+ *   tokens * top_k at most 2^24.
+ *   workspace  at least teal_workspace_bytes_experts(m, sum of n_k, tokens * top_k)
+ *          bytes, zero before first use like every workspace.  No survivor counts.
+ * teal_sparse_experts_{bf16,mx4}_swiglu: the W_down step of the experts,
+ *   y[b] = sum over j of weight[b][j] * s_{t[e]}(h[b][j]) W[e]^T, e = idx[b][j],
+ * h = fp16(SiLU(gate) * up) in the arithmetic stated for teal_sparse_gemv_bf16_swiglu.
+ * A pair without an expert adds nothing, whatever its weight.
+ *   gate, up [tokens][top_k][m] fp32; weight [tokens][top_k] fp32; y [tokens][n].
+ *   m = the experts' width, n = the model width; workspace of
+ *   teal_workspace_bytes_experts(m, n, tokens * top_k).
+ */
+#define TEAL_MAX_EXPERTS 1024
+#define TEAL_MAX_TOP_K 32
+#define TEAL_SCORE_SOFTMAX 0
+#define TEAL_SCORE_SIGMOID 1
+teal_status teal_route_experts(const float *logits, const float *bias, int score, int tokens,
+                               int experts, int groups, int top_groups, int group_top, int top_k,
+                               int renormalise, float scaling, int32_t *idx, float *weight,
+                               void *stream);
+size_t teal_workspace_bytes_experts(int m, int n, int pairs);
+teal_status teal_sparse_experts_bf16(int count, const void *const *Wt_bf16, const float *const *t,
+                                     float *const *y, const int *n, int experts, const int32_t *idx,
+                                     int tokens, int top_k, const void *X_f16, int m,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+teal_status teal_sparse_experts_mx4(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                    const float *const *t, float *const *y, const int *n,
+                                    int experts, const int32_t *idx, int tokens, int top_k,
+                                    const void *X_f16, int m, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+teal_status teal_sparse_experts_bf16_swiglu(const void *Wt_bf16, const float *t, float *y,
+                                            int experts, const int32_t *idx, const float *weight,
+                                            int tokens, int top_k, const float *gate,
+                                            const float *up, int m, int n, void *workspace,
+                                            size_t workspace_bytes, void *stream);
+teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *t,
+                                           float *y, int experts, const int32_t *idx,
+                                           const float *weight, int tokens, int top_k,
+                                           const float *gate, const float *up, int m, int n,
+                                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * The MLP of a Transformer block in ONE kernel launch (Appendix A.3):
  *     MLP(x) = (SiLU(x W_gate^T) . x W_up^T) W_down^T,
  * with every product thresholded (Section 4.2): gate = s_{t_gate}(x) W_gate^T,

@@ -26,4 +26,9 @@ from .binding import (  # noqa: F401
     teal_mlp_plan, teal_mlp_block_info, teal_sparse_mlp_bf16, teal_sparse_mlp_w8, teal_sparse_mlp_w4,
     teal_sparse_gemv_bf16_multi_pitch, teal_sparse_gemv_w8_multi_pitch, teal_gemv_plan_multi_pitch,
     teal_sparse_gemv_bf16_rmsnorm_multi_pitch,
+    teal_mx4_scale_bytes, teal_pack_mx4, teal_unpack_mx4, teal_sparse_gemv_mx4, teal_sparse_gemv_mx4_multi,
+    teal_sparse_gemv_mx4_swiglu, teal_sparse_gemv_mx4_rmsnorm_multi,
+    TEAL_MAX_EXPERTS, TEAL_MAX_TOP_K, TEAL_SCORE_SOFTMAX, TEAL_SCORE_SIGMOID, teal_route_experts,
+    teal_workspace_bytes_experts, teal_sparse_experts_bf16, teal_sparse_experts_mx4,
+    teal_sparse_experts_bf16_swiglu, teal_sparse_experts_mx4_swiglu,
 )

@@ -43,9 +43,17 @@ EXPORTS = (
     "teal_workspace_bytes_mlp", "teal_mlp_down_region_offset", "teal_mlp_status_offset",
     "teal_mlp_plan", "teal_mlp_block_info", "teal_sparse_mlp_bf16", "teal_sparse_mlp_w8",
     "teal_sparse_mlp_w4",
+    "teal_mx4_scale_bytes", "teal_pack_mx4", "teal_unpack_mx4", "teal_sparse_gemv_mx4",
+    "teal_sparse_gemv_mx4_multi", "teal_sparse_gemv_mx4_swiglu", "teal_sparse_gemv_mx4_rmsnorm_multi",
+    "teal_route_experts", "teal_workspace_bytes_experts", "teal_sparse_experts_bf16",
+    "teal_sparse_experts_mx4", "teal_sparse_experts_bf16_swiglu", "teal_sparse_experts_mx4_swiglu",
 )
 TEAL_HIST_BINS = 32768
 TEAL_MAX_BATCH = 8
+TEAL_MAX_EXPERTS = 1024
+TEAL_MAX_TOP_K = 32
+TEAL_SCORE_SOFTMAX = 0
+TEAL_SCORE_SIGMOID = 1
 
 
 class MlpShape(ctypes.Structure):
@@ -200,6 +208,33 @@ def load_library():
     lib.teal_sparse_mlp_w4.restype = i
     lib.teal_sparse_mlp_w4.argtypes = [vp, vp, vp, vp, vp, vp, i, vp, f, f, f, vp, vp, vp, i, i, i,
                                        vp, sz, vp, shp]
+    vpp, fp, ipp = c.POINTER(vp), c.POINTER(f), c.POINTER(i)
+    lib.teal_mx4_scale_bytes.restype = sz
+    lib.teal_mx4_scale_bytes.argtypes = [i, i]
+    lib.teal_pack_mx4.restype = i
+    lib.teal_pack_mx4.argtypes = [vp, vp, vp, i, i, vp]
+    lib.teal_unpack_mx4.restype = i
+    lib.teal_unpack_mx4.argtypes = [vp, vp, vp, i, i, vp]
+    lib.teal_sparse_gemv_mx4.restype = i
+    lib.teal_sparse_gemv_mx4.argtypes = [vp, vp, vp, f, vp, i, i, vp, sz, vp]
+    lib.teal_sparse_gemv_mx4_multi.restype = i
+    lib.teal_sparse_gemv_mx4_multi.argtypes = [i, vpp, vpp, fp, vpp, ipp, vp, i, vp, sz, vp]
+    lib.teal_sparse_gemv_mx4_swiglu.restype = i
+    lib.teal_sparse_gemv_mx4_swiglu.argtypes = [vp, vp, vp, vp, f, vp, i, i, vp, sz, vp]
+    lib.teal_sparse_gemv_mx4_rmsnorm_multi.restype = i
+    lib.teal_sparse_gemv_mx4_rmsnorm_multi.argtypes = [i, vpp, vpp, fp, vpp, ipp, vp, vp, f, i, vp, sz, vp]
+    lib.teal_route_experts.restype = i
+    lib.teal_route_experts.argtypes = [vp, vp, i, i, i, i, i, i, i, i, f, vp, vp, vp]
+    lib.teal_workspace_bytes_experts.restype = sz
+    lib.teal_workspace_bytes_experts.argtypes = [i, i, i]
+    lib.teal_sparse_experts_bf16.restype = i
+    lib.teal_sparse_experts_bf16.argtypes = [i, vpp, vpp, vpp, ipp, i, vp, i, i, vp, i, vp, sz, vp]
+    lib.teal_sparse_experts_mx4.restype = i
+    lib.teal_sparse_experts_mx4.argtypes = [i, vpp, vpp, vpp, vpp, ipp, i, vp, i, i, vp, i, vp, sz, vp]
+    lib.teal_sparse_experts_bf16_swiglu.restype = i
+    lib.teal_sparse_experts_bf16_swiglu.argtypes = [vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp, sz, vp]
+    lib.teal_sparse_experts_mx4_swiglu.restype = i
+    lib.teal_sparse_experts_mx4_swiglu.argtypes = [vp, vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp, sz, vp]
     ip = c.POINTER(c.c_int)
     lib.teal_gemv_plan.restype = i
     lib.teal_gemv_plan.argtypes = [i, i, i, ip, ip, ip, ip, ip]
@@ -835,3 +870,145 @@ def teal_sparse_mlp_w4(Wq_gate, Wq_up, Wq_down, scale_gate, scale_up, scale_down
         _ptr(gate, 4 * f, "gate"), _ptr(up, 4 * f, "up"), _ptr(y, 4 * d, "y"),
         int(m), int(f), int(d), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream), ctypes.pointer(sh) if sh is not None else None)
+
+
+def teal_mx4_scale_bytes(m: int, n: int) -> int:
+    return int(load_library().teal_mx4_scale_bytes(int(m), int(n)))
+
+
+def _mx4_scale_need(m, n):
+    """Bytes of the scales of an [m][n] matrix; what a call with other sizes is refused for is left to it."""
+    return (m + 7) // 8 * ((n + 511) // 512) * 128
+
+
+def teal_pack_mx4(W_rowmajor, Wq, scale, m, n, stream=None) -> int:
+    return _call("teal_pack_mx4", _ptr(W_rowmajor, 2 * m * n, "W"), _ptr(Wq, m * n // 2, "Wq"),
+                 _ptr(scale, _mx4_scale_need(m, n), "scale"), int(m), int(n), _stream(stream))
+
+
+def teal_unpack_mx4(Wq, scale, W_rowmajor, m, n, stream=None) -> int:
+    return _call("teal_unpack_mx4", _ptr(Wq, m * n // 2, "Wq"), _ptr(scale, _mx4_scale_need(m, n), "scale"),
+                 _ptr(W_rowmajor, 2 * m * n, "W"), int(m), int(n), _stream(stream))
+
+
+def teal_sparse_gemv_mx4(Wq, scale, x_f16, t, y, m, n, workspace, workspace_bytes=None, stream=None) -> int:
+    return _call(
+        "teal_sparse_gemv_mx4",
+        _ptr(Wq, m * n // 2, "Wq"), _ptr(scale, _mx4_scale_need(m, n), "scale"), _ptr(x_f16, 2 * m, "x"), float(t),
+        _ptr(y, 4 * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def _mx4_arrays(Wq_list, scale_list, y_list, n_list, m, experts=1, rows=1):
+    """Host arrays of a grouped call; `experts` matrices and `rows` output rows per entry."""
+    count = len(Wq_list)
+    if not (len(scale_list) == len(y_list) == len(n_list) == count):
+        raise ValueError("per-matrix lists must have the same length")
+    W = (ctypes.c_void_p * count)(*[_ptr(w, experts * (m * n // 2), "Wq") for w, n in zip(Wq_list, n_list)])
+    S = (ctypes.c_void_p * count)(*[_ptr(sc, experts * _mx4_scale_need(m, n), "scale")
+                                    for sc, n in zip(scale_list, n_list)])
+    Y = (ctypes.c_void_p * count)(*[_ptr(y, 4 * rows * n, "y") for y, n in zip(y_list, n_list)])
+    N = (ctypes.c_int * count)(*[int(n) for n in n_list])
+    return count, W, S, Y, N
+
+
+def teal_sparse_gemv_mx4_multi(Wq_list, scale_list, t_list, y_list, n_list, x_f16, m, workspace,
+                               workspace_bytes=None, stream=None) -> int:
+    """count = len(Wq_list) microscaled matrices sharing x; the per-matrix lists become host arrays."""
+    count, W, S, Y, N = _mx4_arrays(Wq_list, scale_list, y_list, n_list, m)
+    if len(t_list) != count:
+        raise ValueError("per-matrix lists must have the same length")
+    Tt = (ctypes.c_float * count)(*[float(t) for t in t_list])
+    return _call(
+        "teal_sparse_gemv_mx4_multi",
+        count, W, S, Tt, Y, N, _ptr(x_f16, 2 * m, "x"), int(m), _ptr(workspace),
+        _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_sparse_gemv_mx4_swiglu(Wq, scale, gate, up, t, y, m, n, workspace, workspace_bytes=None,
+                                stream=None) -> int:
+    return _call(
+        "teal_sparse_gemv_mx4_swiglu",
+        _ptr(Wq, m * n // 2, "Wq"), _ptr(scale, _mx4_scale_need(m, n), "scale"), _ptr(gate, 4 * m, "gate"),
+        _ptr(up, 4 * m, "up"), float(t), _ptr(y, 4 * n, "y"), int(m), int(n), _ptr(workspace),
+        _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_sparse_gemv_mx4_rmsnorm_multi(Wq_list, scale_list, t_list, y_list, n_list, h, gamma, eps, m, workspace,
+                                       workspace_bytes=None, stream=None) -> int:
+    count, W, S, Y, N = _mx4_arrays(Wq_list, scale_list, y_list, n_list, m)
+    if len(t_list) != count:
+        raise ValueError("per-matrix lists must have the same length")
+    Tt = (ctypes.c_float * count)(*[float(t) for t in t_list])
+    return _call(
+        "teal_sparse_gemv_mx4_rmsnorm_multi",
+        count, W, S, Tt, Y, N, _ptr(h, 4 * m, "h"), _ptr(gamma, 4 * m, "gamma"), float(eps), int(m),
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_route_experts(logits, bias, score, tokens, experts, groups, top_groups, group_top, top_k, renormalise,
+                       scaling, idx, weight, stream=None) -> int:
+    return _call(
+        "teal_route_experts",
+        _ptr(logits, 4 * tokens * experts, "logits"), _ptr(bias, 4 * experts, "bias"), int(score), int(tokens),
+        int(experts), int(groups), int(top_groups), int(group_top), int(top_k), int(bool(renormalise)),
+        float(scaling), _ptr(idx, 4 * tokens * top_k, "idx"), _ptr(weight, 4 * tokens * top_k, "weight"),
+        _stream(stream))
+
+
+def teal_workspace_bytes_experts(m: int, n: int, pairs: int) -> int:
+    return int(load_library().teal_workspace_bytes_experts(int(m), int(n), int(pairs)))
+
+
+def _expert_thresholds(t_list, count, experts):
+    if len(t_list) != count:
+        raise ValueError("per-matrix lists must have the same length")
+    return (ctypes.c_void_p * count)(*[_ptr(t, 4 * experts, "t") for t in t_list])
+
+
+def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, tokens, top_k, X_f16, m, workspace,
+                             workspace_bytes=None, stream=None) -> int:
+    """len(Wt_list) matrices [experts][m][n_k] on each token's experts; t_list: device arrays [experts]."""
+    count = len(Wt_list)
+    if not (len(y_list) == len(n_list) == count):
+        raise ValueError("per-matrix lists must have the same length")
+    W = (ctypes.c_void_p * count)(*[_ptr(w, 2 * experts * m * n, "Wt") for w, n in zip(Wt_list, n_list)])
+    Y = (ctypes.c_void_p * count)(*[_ptr(y, 4 * tokens * top_k * n, "y") for y, n in zip(y_list, n_list)])
+    N = (ctypes.c_int * count)(*[int(n) for n in n_list])
+    return _call(
+        "teal_sparse_experts_bf16",
+        count, W, _expert_thresholds(t_list, count, experts), Y, N, int(experts),
+        _ptr(idx, 4 * tokens * top_k, "idx"), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_sparse_experts_mx4(Wq_list, scale_list, t_list, y_list, n_list, experts, idx, tokens, top_k, X_f16, m,
+                            workspace, workspace_bytes=None, stream=None) -> int:
+    count, W, S, Y, N = _mx4_arrays(Wq_list, scale_list, y_list, n_list, m, experts, tokens * top_k)
+    return _call(
+        "teal_sparse_experts_mx4",
+        count, W, S, _expert_thresholds(t_list, count, experts), Y, N, int(experts),
+        _ptr(idx, 4 * tokens * top_k, "idx"), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_sparse_experts_bf16_swiglu(Wt_bf16, t, y, experts, idx, weight, tokens, top_k, gate, up, m, n, workspace,
+                                    workspace_bytes=None, stream=None) -> int:
+    pairs = tokens * top_k
+    return _call(
+        "teal_sparse_experts_bf16_swiglu",
+        _ptr(Wt_bf16, 2 * experts * m * n, "Wt"), _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"),
+        int(experts), _ptr(idx, 4 * pairs, "idx"), _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k),
+        _ptr(gate, 4 * pairs * m, "gate"), _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace),
+        _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_sparse_experts_mx4_swiglu(Wq, scale, t, y, experts, idx, weight, tokens, top_k, gate, up, m, n, workspace,
+                                   workspace_bytes=None, stream=None) -> int:
+    pairs = tokens * top_k
+    return _call(
+        "teal_sparse_experts_mx4_swiglu",
+        _ptr(Wq, experts * (m * n // 2), "Wq"), _ptr(scale, experts * _mx4_scale_need(m, n), "scale"),
+        _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _ptr(idx, 4 * pairs, "idx"),
+        _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k), _ptr(gate, 4 * pairs * m, "gate"),
+        _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+        _stream(stream))

@@ -1,6 +1,7 @@
 // y = s_t(x) W^T for bf16 weights stored input-channel-major (Sections 3, 4.2, 4.4).
 #include "gemv_common.h"
 #include "gemv_dispatch.h"
+#include "gemv_experts.h"
 #include "gemv_mlp.h"
 
 namespace teal {
@@ -21,6 +22,11 @@ struct FmtBF16 {
     {
         a.W = take ? b.W : a.W;
         a.ld = take ? b.ld : a.ld;
+    }
+    // The same matrix of expert e, [m][n] matrices one behind the other.
+    static __device__ __forceinline__ void expert(Args &a, int e, int m, int n)
+    {
+        a.W = static_cast<const uint16_t *>(a.W) + (size_t)e * m * n;
     }
     // bf16 -> fp32 is a 16-bit shift; bf16 * fp16 is exact in fp32 (8 + 11 significand bits).
     static __device__ __forceinline__ void fma(float (&acc)[8], u32x4 v, float xv)
@@ -197,6 +203,14 @@ hipError_t launch_mlp_bf16(const MlpHostArgs &h, const MlpLaunch &L, hipStream_t
         return hipErrorInvalidValue;
     return launch_mlp_kernel<GemvBody<FmtBF16>, false>(A, L.gu.lanes_per_row,
                                                        L.down.lanes_per_row, lds, stream);
+}
+
+hipError_t launch_experts_bf16(const ExpertHostArgs &h, const GemvShape &sh, hipStream_t stream)
+{
+    if (!gemv_shape_supported(sh) || sh.lanes_per_row < 16 || sh.waves != 8 || sh.unroll != 4)
+        return hipErrorInvalidValue;
+    return launch_experts<GemvBody<FmtBF16>>(h, sh, stream,
+                                             [](FmtBF16::Args &a, const void *W, const void *) { a.W = W; });
 }
 
 }  // namespace teal

@@ -124,6 +124,7 @@ __device__ __forceinline__ int wave_inclusive_scan(int v)
 // counters: int total[kMaxMatrices] (padded to kReportHeaderInts), then one row of `splits`
 // slice counts per matrix.
 struct SurvivorReport {
+    static constexpr bool kOn = true;
     int *total;        // this matrix's slot
     int *per_split;    // this matrix's row of slice counts
     int matrix;
@@ -165,6 +166,11 @@ __device__ __forceinline__ SurvivorReport survivor_report(int *counters_base, in
     int *area = counters_base + kCounterBytes / sizeof(int);
     return SurvivorReport{area + matrix, area + kReportHeaderInts + matrix * splits, matrix};
 }
+
+// For launches that leave no count.
+struct NoReport {
+    static constexpr bool kOn = false;
+};
 
 // Called by one thread of a block of tile 0 before the block's arrival (or instead of it
 // when there is one split).  Where there are column words the counts have one too, see block_finish.
@@ -885,6 +891,15 @@ __device__ __forceinline__ void store_wave_sums(const float (&acc)[N], float *ds
     }
 }
 
+// What meets in a sum of y: the K-slices of one product.  (Another form, for sums that several products share, is
+// in gemv_experts.h.)
+struct OneProduct {
+    __device__ __forceinline__ int slice(int s) const { return s; }               // of the slices that meet
+    __device__ __forceinline__ int slices(int splits) const { return splits; }
+    __device__ __forceinline__ float grid_threshold(float t) const { return t; }  // the same for all of them
+    __device__ __forceinline__ float sum(float v) const { return v; }             // what a slice's sum counts for
+};
+
 // Sums the wavefronts' accumulators through LDS.  With one split the sums are the outputs.  Otherwise the
 // slices of the tile meet (the split-K combine of Section 4.4, without a second launch), in one of two ways
 // with the same result, which does not depend on the order in which they arrive:
@@ -899,11 +914,11 @@ __device__ __forceinline__ void store_wave_sums(const float (&acc)[N], float *ds
 // wrote (with column words a tile's columns may be written by different blocks).
 // The combine buffer has SUMS rows of combine_row floats, a row per wavefront unless a format
 // says otherwise.
-template <class F, int LPR, int WAVES, int SUMS = WAVES>
+template <class F, int LPR, int WAVES, int SUMS = WAVES, class Report = SurvivorReport, class Join = OneProduct>
 __device__ __forceinline__ int block_finish(float *red, float *partial, const Meeting &meet, int gtile,
                                              float *y, int tile, int col0, int cols, int s, int splits, int n,
-                                             const typename F::Args &a, const SurvivorReport &report, int cnt,
-                                             float t)
+                                             const typename F::Args &a, const Report &report, int cnt,
+                                             float t, const Join &join = Join{})
 {
     constexpr int EPL = F::kElemsPerLane;
     constexpr int TN = LPR * EPL;
@@ -930,7 +945,7 @@ __device__ __forceinline__ int block_finish(float *red, float *partial, const Me
                 float sum = 0.f;
 #pragma unroll
                 for (int ww = 0; ww < SUMS; ++ww) sum += red[ww * ROW + combine_index<EPL, LPR>(c)];
-                store_coherent(y + col0 + c, F::finish(sum, scale[k]));
+                store_coherent(y + col0 + c, F::finish(join.sum(sum), scale[k]));
                 ++wrote;
             }
         }
@@ -942,7 +957,7 @@ __device__ __forceinline__ int block_finish(float *red, float *partial, const Me
         float sum = 0.f;
 #pragma unroll
         for (int ww = 0; ww < SUMS; ++ww) sum += red[ww * ROW + combine_index<EPL, LPR>(c)];
-        return sum;
+        return join.sum(sum);
     };
     const Grid grid{F::grid_unit(t), splits};
     if (meet.word_step) {
@@ -956,10 +971,14 @@ __device__ __forceinline__ int block_finish(float *red, float *partial, const Me
                 found[k] = word_add(words.word + c, mine[k]);
             }
         }
-        unsigned long long *const counts = count_word(meet, report.matrix);
-        const bool reports = tile == 0 && threadIdx.x == (WAVES - 1) * 64;
+        unsigned long long *counts = nullptr;
+        bool reports = false;
         unsigned long long counted = 0;
-        if (reports) counted = count_slice(counts, cnt);
+        if constexpr (Report::kOn) {
+            counts = count_word(meet, report.matrix);
+            reports = tile == 0 && threadIdx.x == (WAVES - 1) * 64;
+            if (reports) counted = count_slice(counts, cnt);
+        }
         trace_mark(4);
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
@@ -970,7 +989,9 @@ __device__ __forceinline__ int block_finish(float *red, float *partial, const Me
                 ++wrote;
             }
         }
-        if (reports) count_total(report, counts, cnt, splits, counted);
+        if constexpr (Report::kOn) {
+            if (reports) count_total(report, counts, cnt, splits, counted);
+        }
         trace_mark(5);
         return wrote;
     }
@@ -1004,7 +1025,9 @@ __device__ __forceinline__ int block_finish(float *red, float *partial, const Me
     if (!last_flag) return 0;
     // (by a wavefront that has no columns where there is one: ahead of the first wavefront's partial rows
     // its loads made tile 0 the last to end, 1.0 us after its ticket against 0.76 for the others)
-    if (tile == 0 && w == WAVES - 1) report_total(report, splits);
+    if constexpr (Report::kOn) {
+        if (tile == 0 && w == WAVES - 1) report_total(report, splits);
+    }
 
     // Second pass.  A thread owns a column and adds its partial rows in split order (a fixed
     // order, whichever block happens to be last), 8 or 16 loads in flight at once.  (Spreading
@@ -1085,11 +1108,11 @@ __device__ __forceinline__ int lane_column(int col0, int cols, int n, int l)
 // Work of one block for formats with no per-group state (bf16, int8): output
 // tile `tile` (tile_cols columns) x K-slice `s` (ks channels) of one matrix.
 // Returns how many of the tile's outputs this thread wrote.
-template <class F, int LPR, int WAVES, int U, class XS>
+template <class F, int LPR, int WAVES, int U, class XS, class Report = SurvivorReport, class Join = OneProduct>
 __device__ __forceinline__ int gemv_block(const typename F::Args &a, const XS &x,
                                            float t, float *partial, const Meeting &meet, int gtile,
                                            float *y, int m, int n, int ks, int tile, int s, int tile_cols,
-                                           int splits, const SurvivorReport &report)
+                                           int splits, const Report &report, const Join &join = Join{})
 {
     constexpr int EPL = F::kElemsPerLane;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -1123,7 +1146,9 @@ __device__ __forceinline__ int gemv_block(const typename F::Args &a, const XS &x
     }
 
     trace_mark(2);
-    if (tile == 0 && !meet.word_step && threadIdx.x == (WAVES - 1) * 64) report_slice(report, s, splits, cnt);
+    if constexpr (Report::kOn) {
+        if (tile == 0 && !meet.word_step && threadIdx.x == (WAVES - 1) * 64) report_slice(report, s, splits, cnt);
+    }
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int start, mine;
@@ -1142,8 +1167,8 @@ __device__ __forceinline__ int gemv_block(const typename F::Args &a, const XS &x
     trace_mark(3);
     trace_mark_thread(1, (WAVES - 1) * 64);
     store_wave_sums<LPR>(acc, red + (threadIdx.x >> 6) * combine_row<EPL, LPR>);
-    return block_finish<F, LPR, WAVES>(red, partial, meet, gtile, y, tile, col0, tile_cols, s, splits, n, a,
-                                       report, cnt, t);
+    return block_finish<F, LPR, WAVES>(red, partial, meet, gtile, y, tile, col0, tile_cols, join.slice(s),
+                                       join.slices(splits), n, a, report, cnt, join.grid_threshold(t), join);
 }
 
 // One matrix per launch.  Grid: tiles x splits blocks (two dimensions: a division of the block index

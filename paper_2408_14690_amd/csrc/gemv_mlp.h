@@ -78,14 +78,14 @@ struct MlpArgs {
 template <class F>
 struct GemvBody {
     typedef F Format;
-    template <int LPR, class XS>
+    template <int LPR, class XS, class Report, class Join = OneProduct>
     static __device__ __forceinline__ int run(const typename F::Args &a, const XS &x, float t,
                                                float *partial, const Meeting &meet, int gtile, float *y, int m,
                                                int n, int ks, int tile, int s, int tile_cols,
-                                               int splits, const SurvivorReport &report)
+                                               int splits, const Report &report, const Join &join = Join{})
     {
         return gemv_block<F, LPR, 8, 4>(a, x, t, partial, meet, gtile, y, m, n, ks, tile, s,
-                                        tile_cols, splits, report);
+                                        tile_cols, splits, report, join);
     }
 };
 

@@ -1,0 +1,464 @@
+// y = s_t(x) W^T for microscaled 4-bit weights: blocks of 32 neighbouring outputs of one input channel share a
+// power of two, W[j][i] = level(code(i, j)) * 2^(scale(i, j / 32) - 127), level one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+// and a sign.  The blocks lie along the outputs, not along the sum: a channel that is dropped takes its scales
+// with it, and a lane's 16 bytes are one block with one scale.
+//
+// Scales are stored in tiles of 8 channels by 16 blocks, 128 bytes: what an output tile of 512 columns reads of
+// a channel's scales are 16 bytes, and a row of them would be a line that the tiles beside it, on other XCDs,
+// fetch too; of a tile of scales the line's other bytes belong to the next channels of the same block.
+#include <type_traits>
+
+#include "gemv_common.h"
+#include "gemv_experts.h"
+#include "gemv_mlp.h"
+
+namespace teal {
+
+struct FmtMx4 {
+    static constexpr int kElemsPerLane = 32;   // 16 bytes = 32 codes, one block
+    static constexpr int kBitsPerElem = 4;
+    // scales of any size, as bf16 weights
+    static __device__ __forceinline__ int grid_unit(float t) { return grid_unit_bf16(t); }
+    struct Args {
+        const void *W;
+        const unsigned char *scale;
+    };
+    static __device__ __forceinline__ void select(Args &a, const Args &b, bool take)
+    {
+        a.W = take ? b.W : a.W;
+        a.scale = take ? b.scale : a.scale;
+    }
+    // The same matrix of expert e, [m][n] matrices one behind the other.
+    static __device__ __forceinline__ void expert(Args &a, int e, int m, int n)
+    {
+        a.W = static_cast<const unsigned char *>(a.W) + (size_t)e * m * (n / 2);
+        a.scale += (size_t)e * mx4_scale_bytes(m, n);
+    }
+    static __device__ __forceinline__ void read_now(const Args (&a)[4])
+    {
+        asm volatile("" ::"s"(a[0].scale), "s"(a[1].scale), "s"(a[2].scale), "s"(a[3].scale));
+    }
+    struct ColumnScale {};
+    static __device__ __forceinline__ ColumnScale column_scale(const Args &, int) { return {}; }
+    static __device__ __forceinline__ float finish(float sum, ColumnScale) { return sum; }
+
+    // The conversion scales by the exponent of an fp32 number: exact, and NaN for the scale byte 255.
+    static __device__ __forceinline__ void fma(float (&acc)[32], u32x4 v, unsigned scale, float xv)
+    {
+        const float sc = __uint_as_float(scale << 23);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#define TEAL_PAIR(B)                                                                           \
+    do {                                                                                       \
+        const auto w = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[q], sc, B);                  \
+        acc[8 * q + 2 * B] = fmaf(xv, w[0], acc[8 * q + 2 * B]);                               \
+        acc[8 * q + 2 * B + 1] = fmaf(xv, w[1], acc[8 * q + 2 * B + 1]);                       \
+    } while (0)
+            TEAL_PAIR(0);
+            TEAL_PAIR(1);
+            TEAL_PAIR(2);
+            TEAL_PAIR(3);
+#undef TEAL_PAIR
+        }
+    }
+};
+
+constexpr int kMx4Waves = 8;
+constexpr int kMx4Unroll = 4;
+constexpr int kMx4Lanes = 16;
+
+template <int U>
+struct Mx4Batch {
+    u32x4 v[U];
+    unsigned sc[U];
+    float xv[U];
+};
+
+// Work of one block: output tile `tile` (tile_cols columns, at most 512) x K-slice `s` (ks channels).  16 lanes share a
+// row, four rows per wavefront load; the wavefronts take equal contiguous shares of the compacted list, two
+// batches of loads in flight (as stream_rows).  Returns how many of the tile's outputs this thread wrote.
+template <int LPR, int WAVES, int U, class XS, class Report = SurvivorReport, class Join = OneProduct>
+__device__ __forceinline__ int mx4_block(const FmtMx4::Args &a, const XS &x, float t, float *partial,
+                                          const Meeting &meet, int gtile, float *y, int m, int n, int ks, int tile,
+                                          int s, int tile_cols, int splits, const Report &report,
+                                          const Join &join = Join{})
+{
+    using F = FmtMx4;
+    constexpr int EPL = F::kElemsPerLane;
+    constexpr int R = 64 / LPR;
+    extern __shared__ __align__(16) unsigned char smem[];
+    int2 *list = reinterpret_cast<int2 *>(smem);
+    float *red = reinterpret_cast<float *>(smem + (size_t)ks * sizeof(int2));
+    __shared__ int counts[kCompactInts];
+
+    asm volatile("" ::"s"(a.W), "s"(a.scale), "s"(partial), "s"(meet.counters), "s"(y));   // as in gemv_block
+    const int k0 = s * ks;
+    const int k1 = min(m, k0 + ks);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int group_excl;
+    int cnt = 0;
+    bool compacted = false;
+    if constexpr (XS::kPlainHalf) {
+        if (k1 - k0 <= kPrivateSlice) {         // block-uniform: short slices need no barrier
+            cnt = compact_slice_private(x.x, t, k0, k1, w, WAVES, list, group_excl);
+            compacted = true;
+        }
+    }
+    if (!compacted) cnt = compact_slice<WAVES>(x, t, k0, k1, list, counts, group_excl);
+
+    trace_mark(2);
+    if constexpr (Report::kOn) {
+        if (tile == 0 && !meet.word_step && threadIdx.x == (WAVES - 1) * 64) report_slice(report, s, splits, cnt);
+    }
+    const int lane = threadIdx.x & 63;
+    const int g = lane / LPR;
+    const int col0 = tile * tile_cols;
+    const int col = lane_column<EPL>(col0, tile_cols, n, lane % LPR);
+    const unsigned row_bytes = (unsigned)(n / 2);
+    const unsigned char *lane_base = static_cast<const unsigned char *>(a.W) + col / 2;
+    const unsigned tiles_bytes = (unsigned)mx4_scale_tiles(n) * kMx4TileBytes;      // of 8 channels' scales
+    const unsigned char *scale_base = a.scale + (col / 512) * kMx4TileBytes + col / 32 % 16;
+
+    float acc[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+    int start, mine;
+    wave_share(cnt, w, WAVES, start, mine);
+    if (mine > 0) {
+        const int last = mine - 1;
+        const int batches = (mine + U * R - 1) / (U * R);
+        // slots past the end of the share repeat the last row with a zero multiplier
+        auto issue = [&](Mx4Batch<U> &b, int batch) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = (batch * U + u) * R + g;
+                const int2 ent = list[start + min(e, last)];
+                const unsigned i = (unsigned)ent.x;
+                b.xv[u] = e <= last ? __int_as_float(ent.y) : 0.f;
+                b.v[u] = load_stream16(lane_base + (size_t)i * row_bytes);
+                b.sc[u] = scale_base[(size_t)(i / 8) * tiles_bytes + i % 8 * 16];
+            }
+        };
+        auto consume = [&](const Mx4Batch<U> &b) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) F::fma(acc, b.v[u], b.sc[u], b.xv[u]);
+        };
+        Mx4Batch<U> b0, b1;
+        issue(b0, 0);
+        int it = 0;
+        for (; it + 2 < batches; it += 2) {
+            issue(b1, it + 1);
+            consume(b0);
+            issue(b0, it + 2);
+            consume(b1);
+        }
+        if (it + 1 < batches) {
+            issue(b1, it + 1);
+            consume(b0);
+            consume(b1);
+        } else {
+            consume(b0);
+        }
+    }
+    trace_mark(3);
+    trace_mark_thread(1, (WAVES - 1) * 64);
+    store_wave_sums<LPR>(acc, red + w * combine_row<EPL, LPR>);
+    return block_finish<F, LPR, WAVES>(red, partial, meet, gtile, y, tile, col0, tile_cols, join.slice(s),
+                                       join.slices(splits), n, a, report, cnt, join.grid_threshold(t), join);
+}
+
+struct Mx4Body {
+    typedef FmtMx4 Format;
+    template <int LPR, class XS, class Report, class Join = OneProduct>
+    static __device__ __forceinline__ int run(const FmtMx4::Args &a, const XS &x, float t, float *partial,
+                                               const Meeting &meet, int gtile, float *y, int m, int n, int ks,
+                                               int tile, int s, int tile_cols, int splits, const Report &report,
+                                               const Join &join = Join{})
+    {
+        return mx4_block<LPR, kMx4Waves, kMx4Unroll>(a, x, t, partial, meet, gtile, y, m, n, ks, tile, s, tile_cols,
+                                                     splits, report, join);
+    }
+};
+
+__global__ __launch_bounds__(kMx4Waves * 64) void sparse_gemv_mx4_kernel(
+    FmtMx4::Args a, const __half *__restrict__ x, float t, float *partial, Meeting meet, float *y, int m, int n,
+    int ks, int tile_cols, int splits)
+{
+    trace_mark(0);
+    const int tile = blockIdx.x;
+    Mx4Body::run<kMx4Lanes>(a, HalfSource{x}, t, partial, meet, tile, y, m, n, ks, tile, blockIdx.y, tile_cols, splits,
+                            survivor_report(meet.counters, 0, splits));
+    trace_mark(6);
+}
+
+// The input formed from the two products that precede W_down, as in sparse_gemv_swiglu_kernel.
+__global__ __launch_bounds__(kMx4Waves * 64) void sparse_gemv_mx4_swiglu_kernel(
+    FmtMx4::Args a, const float *__restrict__ gate, const float *__restrict__ up, float t, float *partial,
+    Meeting meet, float *y, int m, int n, int ks, int tile_cols, int splits)
+{
+    trace_mark(0);
+    const int tile = blockIdx.x;
+    Mx4Body::run<kMx4Lanes>(a, SwigluSource{gate, up}, t, partial, meet, tile, y, m, n, ks, tile, blockIdx.y, tile_cols,
+                            splits, survivor_report(meet.counters, 0, splits));
+}
+
+// Several matrices that read the same state; the block finds its matrix as in multi_block.
+template <class XS>
+__device__ __forceinline__ void mx4_multi_block(const MultiArgs<FmtMx4> &ma, const XS &x, float *partial,
+                                                const Meeting &meet, int m, int ks, int tile_cols, int splits,
+                                                int gtile, int s)
+{
+    trace_mark(0);
+    int k = 0, first = 0, n = ma.n[0];
+    size_t partial_off = 0;
+    FmtMx4::Args a = ma.a[0];
+    float *y = ma.y[0];
+    float t = ma.t[0];
+    asm volatile("" ::"s"(ma.y[0]), "s"(ma.y[1]), "s"(ma.y[2]), "s"(ma.y[3]), "s"(ma.n[0]), "s"(ma.n[1]),
+                 "s"(ma.n[2]), "s"(ma.n[3]), "s"(ma.t[0]), "s"(ma.t[1]), "s"(ma.t[2]), "s"(ma.t[3]),
+                 "s"(ma.a[0].W), "s"(ma.a[1].W), "s"(ma.a[2].W), "s"(ma.a[3].W), "s"(ma.tile_begin[4]),
+                 "s"(partial), "s"(meet.counters), "s"(splits));
+    FmtMx4::read_now(ma.a);
+#pragma unroll
+    for (int j = 1; j < kMaxMulti; ++j) {
+        const bool here = j < ma.count && gtile >= ma.tile_begin[j];
+        partial_off += here ? (size_t)splits * ma.n[j - 1] : 0;
+        k = here ? j : k;
+        first = here ? ma.tile_begin[j] : first;
+        n = here ? ma.n[j] : n;
+        y = here ? ma.y[j] : y;
+        t = here ? ma.t[j] : t;
+        FmtMx4::select(a, ma.a[j], here);
+    }
+    Mx4Body::run<kMx4Lanes>(a, x, t, partial + partial_off, meet, gtile, y, m, n, ks, gtile - first, s, tile_cols,
+                            splits, survivor_report(meet.counters, k, splits));
+    trace_mark(6);
+}
+
+__global__ __launch_bounds__(kMx4Waves * 64) void sparse_gemv_mx4_multi_kernel(
+    MultiArgs<FmtMx4> ma, const __half *__restrict__ x, float *partial, Meeting meet, int m, int ks, int tile_cols,
+    int splits)
+{
+    asm volatile("" ::"s"(x));                 // as in multi_block
+    mx4_multi_block(ma, HalfSource{x}, partial, meet, m, ks, tile_cols, splits, (int)blockIdx.x, (int)blockIdx.y);
+}
+
+__global__ __launch_bounds__(kNormWaves * 64) void sparse_gemv_mx4_rmsnorm_multi_kernel(
+    MultiArgs<FmtMx4> ma, const float *__restrict__ h, const float *__restrict__ gamma, float eps, double inv_m,
+    float *partial, Meeting meet, int m, int ks, int tile_cols, int splits)
+{
+    static_assert(kMx4Waves == kNormWaves, "the normalisation's scale is formed by a block of kNormWaves");
+    __shared__ double wave_sums[kMaxNormChunks * kNormWaves];
+    asm volatile("" ::"s"(h), "s"(gamma), "s"(eps), "s"(inv_m));      // as in multi_block
+    mx4_multi_block(ma, RmsnormSource{h, gamma, m, inv_m, eps, wave_sums}, partial, meet, m, ks, tile_cols, splits,
+                    (int)blockIdx.x, (int)blockIdx.y);
+}
+
+static bool mx4_shape_ok(const GemvShape &sh)
+{
+    return sh.lanes_per_row == kMx4Lanes && sh.waves == kMx4Waves && sh.unroll == kMx4Unroll && sh.splits >= 1 &&
+           sh.tile_cols > 0 && sh.tile_cols % FmtMx4::kElemsPerLane == 0 &&
+           sh.tile_cols <= kMx4Lanes * FmtMx4::kElemsPerLane;
+}
+
+hipError_t launch_gemv_mx4(const uint8_t *Wq, const uint8_t *scale, const void *x_f16, float t, float *y, int m,
+                           int n, float *partial, int *counters, const GemvShape &sh, hipStream_t stream)
+{
+    if (!mx4_shape_ok(sh)) return hipErrorInvalidValue;
+    const GemvGeometry g = gemv_geometry(m, n, sh, FmtMx4::kElemsPerLane, 64);
+    const Meeting meet = meeting_of(counters, g.tiles, g.tile_cols, g.splits);
+    hipLaunchKernelGGL(sparse_gemv_mx4_kernel, dim3(g.tiles, g.splits), dim3(kMx4Waves * 64), g.lds, stream,
+                       (FmtMx4::Args{Wq, scale}), static_cast<const __half *>(x_f16), t, partial, meet, y, m, n, g.ks,
+                       g.tile_cols, g.splits);
+    return hipGetLastError();
+}
+
+hipError_t launch_gemv_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *gate, const float *up,
+                                  float t, float *y, int m, int n, float *partial, int *counters,
+                                  const GemvShape &sh, hipStream_t stream)
+{
+    if (!mx4_shape_ok(sh)) return hipErrorInvalidValue;
+    const GemvGeometry g = gemv_geometry(m, n, sh, FmtMx4::kElemsPerLane, 64);
+    const Meeting meet = meeting_of(counters, g.tiles, g.tile_cols, g.splits);
+    hipLaunchKernelGGL(sparse_gemv_mx4_swiglu_kernel, dim3(g.tiles, g.splits), dim3(kMx4Waves * 64), g.lds, stream,
+                       (FmtMx4::Args{Wq, scale}), gate, up, t, partial, meet, y, m, n, g.ks, g.tile_cols, g.splits);
+    return hipGetLastError();
+}
+
+static MultiArgs<FmtMx4> mx4_multi_args(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                        const float *t, float *const *y, const int *n, int tile_cols)
+{
+    MultiArgs<FmtMx4> ma{};
+    ma.count = count;
+    for (int k = 0; k < count; ++k) {
+        ma.a[k] = FmtMx4::Args{Wq[k], scale[k]};
+        ma.y[k] = y[k];
+        ma.t[k] = t[k];
+        ma.n[k] = n[k];
+        ma.tile_begin[k + 1] = ma.tile_begin[k] + (n[k] + tile_cols - 1) / tile_cols;
+    }
+    return ma;
+}
+
+hipError_t launch_gemv_mx4_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale, const float *t,
+                                 float *const *y, const int *n, const void *x_f16, int m, float *partial,
+                                 int *counters, const GemvShape &sh, hipStream_t stream)
+{
+    if (!mx4_shape_ok(sh)) return hipErrorInvalidValue;
+    const GemvGeometry g = gemv_geometry(m, n[0], sh, FmtMx4::kElemsPerLane, 64);
+    const MultiArgs<FmtMx4> ma = mx4_multi_args(count, Wq, scale, t, y, n, g.tile_cols);
+    const int tiles = ma.tile_begin[count];
+    const Meeting meet = meeting_of(counters, tiles, g.tile_cols, g.splits);
+    hipLaunchKernelGGL(sparse_gemv_mx4_multi_kernel, dim3(tiles, g.splits), dim3(kMx4Waves * 64), g.lds, stream, ma,
+                       static_cast<const __half *>(x_f16), partial, meet, m, g.ks, g.tile_cols, g.splits);
+    return hipGetLastError();
+}
+
+hipError_t launch_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                         const float *t, float *const *y, const int *n, const float *h,
+                                         const float *gamma, float eps, int m, float *partial, int *counters,
+                                         const GemvShape &sh, hipStream_t stream)
+{
+    if (m < 8 || m > kMaxNormDim || m % 8 != 0 || !mx4_shape_ok(sh)) return hipErrorInvalidValue;
+    const GemvGeometry g = gemv_geometry(m, n[0], sh, FmtMx4::kElemsPerLane, 64);
+    const MultiArgs<FmtMx4> ma = mx4_multi_args(count, Wq, scale, t, y, n, g.tile_cols);
+    const int tiles = ma.tile_begin[count];
+    const Meeting meet = meeting_of(counters, tiles, g.tile_cols, g.splits);
+    hipLaunchKernelGGL(sparse_gemv_mx4_rmsnorm_multi_kernel, dim3(tiles, g.splits), dim3(kNormWaves * 64), g.lds,
+                       stream, ma, h, gamma, eps, 1.0 / m, partial, meet, m, g.ks, g.tile_cols, g.splits);
+    return hipGetLastError();
+}
+
+hipError_t launch_experts_mx4(const ExpertHostArgs &h, const GemvShape &sh, hipStream_t stream)
+{
+    if (!mx4_shape_ok(sh)) return hipErrorInvalidValue;
+    return launch_experts<Mx4Body>(h, sh, stream, [](FmtMx4::Args &a, const void *W, const void *scale) {
+        a.W = W;
+        a.scale = static_cast<const unsigned char *>(scale);
+    });
+}
+
+// ---- the format itself: bf16 weights in and out ----
+
+// One thread block lays out 64 channels by 256 outputs: the weights of an output are contiguous along the
+// channels, the codes of a channel along the outputs, so they are turned through LDS.  A thread then has one block
+// of 32 outputs of one channel in two pieces of 16.
+constexpr int kMx4PackRows = 64, kMx4PackCols = 256;
+
+__device__ __forceinline__ unsigned mx4_code(float a, unsigned sign)
+{
+    // nearest level, ties to the even code; a is at most 8
+    const unsigned c = (unsigned)(a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) +
+                       (a > 5.f);
+    return c | sign << 3;
+}
+
+__global__ __launch_bounds__(256) void pack_mx4_kernel(const uint16_t *__restrict__ W, uint8_t *__restrict__ Wq,
+                                                       uint8_t *__restrict__ scale, int m, int n, int tiles_m)
+{
+    __shared__ uint16_t tile[kMx4PackCols][kMx4PackRows + 2];
+    const int i0 = (int)(blockIdx.x % tiles_m) * kMx4PackRows;
+    const int j0 = (int)(blockIdx.x / tiles_m) * kMx4PackCols;
+    const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
+    for (int r = r0; r < kMx4PackCols; r += 4) {
+        const int j = j0 + r, i = i0 + c;
+        tile[r][c] = j < n && i < m ? W[(size_t)j * m + i] : 0;
+    }
+    __syncthreads();
+    for (int b = r0; b < kMx4PackCols / 32; b += 4) {       // channel i0 + c, block b of the tile
+        const int i = i0 + c, j = j0 + 32 * b;
+        if (j >= n) break;
+        unsigned largest = 0;
+        for (int k = 0; k < 32; ++k) largest = max(largest, (unsigned)tile[32 * b + k][c] & 0x7FFFu);
+        // floor(log2) of the largest magnitude, of subnormal ones by their leading bit
+        int e;
+        if (largest >= 0x80u) e = (int)(largest >> 7) - 127;
+        else e = 31 - __clz((int)max(largest, 1u)) - 133;
+        const bool finite = largest < 0x7F80u;
+        const int s = finite ? max(e - 2 + 127, 0) : 255;
+        u32x4 codes = {0u, 0u, 0u, 0u};
+        if (finite) {
+            for (int k = 0; k < 32; ++k) {
+                const unsigned h = tile[32 * b + k][c];
+                const float a = ldexpf(__uint_as_float((h & 0x7FFFu) << 16), 127 - s);
+                codes[k / 8] |= mx4_code(a, h >> 15) << 4 * (k % 8);
+            }
+        }
+        if (i < m) *reinterpret_cast<u32x4 *>(Wq + (size_t)i * (n / 2) + j / 2) = codes;
+        // past the last channel of a tile of scales: zeros
+        if (i < (m + 7) / 8 * 8)
+            scale[((size_t)(i / 8) * mx4_scale_tiles(n) + j / 512) * kMx4TileBytes + i % 8 * 16 + j / 32 % 16] =
+                i < m ? (uint8_t)s : 0;
+    }
+    // past the last block of a tile of scales
+    if (j0 + kMx4PackCols >= n) {
+        const int blocks = n / 32, end = (blocks + 15) / 16 * 16;
+        for (int b = blocks + r0; b < end; b += 4) {
+            const int i = i0 + c;
+            if (i < (m + 7) / 8 * 8)
+                scale[((size_t)(i / 8) * mx4_scale_tiles(n) + b / 16) * kMx4TileBytes + i % 8 * 16 + b % 16] = 0;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void unpack_mx4_kernel(const uint8_t *__restrict__ Wq,
+                                                         const uint8_t *__restrict__ scale, uint16_t *__restrict__ W,
+                                                         int m, int n, int tiles_m)
+{
+    __shared__ uint16_t tile[kMx4PackCols][kMx4PackRows + 2];
+    const int i0 = (int)(blockIdx.x % tiles_m) * kMx4PackRows;
+    const int j0 = (int)(blockIdx.x / tiles_m) * kMx4PackCols;
+    const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
+    for (int b = r0; b < kMx4PackCols / 32; b += 4) {
+        const int i = i0 + c, j = j0 + 32 * b;
+        if (j >= n || i >= m) break;
+        const u32x4 codes = *reinterpret_cast<const u32x4 *>(Wq + (size_t)i * (n / 2) + j / 2);
+        const unsigned s = scale[((size_t)(i / 8) * mx4_scale_tiles(n) + j / 512) * kMx4TileBytes + i % 8 * 16 +
+                                 j / 32 % 16];
+        const float x = __uint_as_float(s << 23);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#define TEAL_PAIR(B)                                                                           \
+    do {                                                                                       \
+        const unsigned w = __builtin_bit_cast(                                                 \
+            unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], x, B));              \
+        tile[32 * b + 8 * q + 2 * B][c] = (uint16_t)w;                                         \
+        tile[32 * b + 8 * q + 2 * B + 1][c] = (uint16_t)(w >> 16);                             \
+    } while (0)
+            TEAL_PAIR(0);
+            TEAL_PAIR(1);
+            TEAL_PAIR(2);
+            TEAL_PAIR(3);
+#undef TEAL_PAIR
+        }
+    }
+    __syncthreads();
+    for (int r = r0; r < kMx4PackCols; r += 4) {
+        const int j = j0 + r, i = i0 + c;
+        if (j < n && i < m) W[(size_t)j * m + i] = tile[r][c];
+    }
+}
+
+hipError_t launch_pack_mx4(const void *W, uint8_t *Wq, uint8_t *scale, int m, int n, hipStream_t stream)
+{
+    const long long tiles_m = (m + kMx4PackRows - 1) / kMx4PackRows, tiles_n = (n + kMx4PackCols - 1) / kMx4PackCols;
+    if (tiles_m * tiles_n > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(pack_mx4_kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, stream,
+                       static_cast<const uint16_t *>(W), Wq, scale, m, n, (int)tiles_m);
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W, int m, int n, hipStream_t stream)
+{
+    const long long tiles_m = (m + kMx4PackRows - 1) / kMx4PackRows, tiles_n = (n + kMx4PackCols - 1) / kMx4PackCols;
+    if (tiles_m * tiles_n > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(unpack_mx4_kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, stream, Wq, scale,
+                       static_cast<uint16_t *>(W), m, n, (int)tiles_m);
+    return hipGetLastError();
+}
+
+}  // namespace teal
+
+#ifdef TEAL_TRACE_BLOCKS
+extern "C" int teal_trace_read_mx4(unsigned long long *host, size_t count) { return teal::read_trace(host, count); }
+#endif

@@ -181,6 +181,76 @@ GemvShape w4_shape(int m, int n)
     sh.splits = (m + ks - 1) / ks;
     return sh;
 }
+// Microscaled 4-bit weights have tiles of up to 512 columns, as narrow as int4's narrowest, and the same idle units
+// where one matrix has few of them.  (Their groups of one are one matrix: there is no stack call to match.)
+GemvShape mx4_shape(int m, const int *n, int count)
+{
+    if (count > 1)
+        return shape_for_multi(m, n, count, 32, 16, 16, 64, teal::kMaxSlice, false);
+    GemvShape sh = auto_shape(m, n[0], 32, 16, 16, 64);
+    const int tiles = (n[0] + sh.tile_cols - 1) / sh.tile_cols;
+    if (tiles * sh.splits > 160) return sh;
+    int splits = kComputeUnits / tiles;
+    if (splits > teal::kWordSplits) splits = teal::kWordSplits;
+    if (splits > m / 128) splits = m / 128;
+    if (splits <= sh.splits) return sh;
+    const int ks = ((m + splits - 1) / splits + 63) / 64 * 64;
+    sh.splits = (m + ks - 1) / ks;
+    return sh;
+}
+
+// The products of `copies` (token, expert) pairs, each with `count` matrices; `joined` of them meet in one sum of y.
+// As shape_for_multi, with several rounds of blocks allowed (a batch's pairs alone may be more than the units)
+// and no more slices to a sum than meet in column words.
+GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, int elems_per_lane, int min_cols,
+                        int step, int max_lanes)
+{
+    double best = -1.0;
+    GemvShape sh{16, 1, 16 * elems_per_lane, 8, 4};
+    long long n_total = 0;
+    for (int k = 0; k < count; ++k) n_total += n[k];
+    for (int tc = max_lanes * elems_per_lane; tc >= min_cols; tc -= step) {
+        long long tiles = 0;
+        for (int k = 0; k < count; ++k) tiles += (n[k] + tc - 1) / tc;
+        for (int splits = 1; splits <= 16; ++splits) {
+            if (splits > 1 && splits > (m + 127) / 128) break;
+            int ks = (m + splits - 1) / splits;
+            ks = (ks + 63) / 64 * 64;
+            if (ks > teal::kMaxSlice) continue;
+            const int s = (m + ks - 1) / ks;
+            const long long blocks = tiles * s * copies;
+            if (s * joined > 1 && tiles * copies > (long long)(teal::kCounterBytes / sizeof(int))) continue;
+            if (s > 1 && blocks > kComputeUnits && m <= teal::kMaxSlice) continue;
+            const long long rounds = (blocks + kComputeUnits - 1) / kComputeUnits;
+            double score = (double)n_total * copies * m / ((double)kComputeUnits * rounds * tc * ks);
+            for (int e = 8; e < s; ++e) score *= 0.97;
+            if (s * joined > teal::kWordSplits) score *= 0.9;
+            if (score > best * 1.001) {
+                best = score;
+                sh.tile_cols = tc;
+                sh.splits = s;
+            }
+        }
+    }
+    if (best < 0.0) {                      // longer than 16 slices
+        sh.tile_cols = 16 * elems_per_lane;
+        sh.splits = (m + teal::kMaxSlice - 1) / teal::kMaxSlice;
+    }
+    while (sh.lanes_per_row * elems_per_lane < sh.tile_cols) sh.lanes_per_row *= 2;
+    return sh;
+}
+
+// Partial rows of such a launch, in floats; `columns` of all pairs together, each with a row per slice.  With more
+// than one slice there are at most kComputeUnits blocks of 512 columns, unless the input is longer than one
+// slice may be.
+size_t experts_partial_floats(int m, long long columns)
+{
+    const size_t resident = (size_t)kComputeUnits * 512;
+    const int forced = (m + teal::kMaxSlice - 1) / teal::kMaxSlice;
+    const size_t rows = (size_t)(forced > 16 ? forced : forced > 1 ? 16 : 1) * columns;
+    return rows > resident ? rows : resident;
+}
+
 GemvShape auto_shape_multi(int m, const int *n, int count, int elems_per_lane, int min_lanes,
                            int max_lanes, int ks_multiple, const int *row_pitch = nullptr)
 {
@@ -1138,6 +1208,256 @@ teal_status teal_sparse_gemv_w4_multi(int count, const uint8_t *const *Wq,
     return from_hip(teal::launch_gemv_w4_multi(count, Wq, scale_f16, t, y, n, x_f16, m,
                                                ws_partials(workspace, m), ws_counters(workspace), sh,
                                                static_cast<hipStream_t>(stream)));
+}
+
+// ---- microscaled 4-bit weights ----
+
+size_t teal_mx4_scale_bytes(int m, int n)
+{
+    if (m < 1 || m > teal::kMaxDim || n < 32 || n > teal::kMaxDim || n % 32 != 0) return 0;
+    return teal::mx4_scale_bytes(m, n);
+}
+
+static teal_status check_mx4_layout(const void *W, const void *Wq, const void *scale, int m, int n)
+{
+    if (!W || !Wq || !scale) return TEAL_ERR_NULL;
+    if (m < 1 || m > teal::kMaxDim || n < 32 || n > teal::kMaxDim || n % 32 != 0) return TEAL_ERR_SHAPE;
+    if (!aligned(W, 2) || !aligned(Wq, 16) || !aligned(scale, 16)) return TEAL_ERR_ALIGN;
+    return TEAL_OK;
+}
+
+teal_status teal_pack_mx4(const void *W_rowmajor, uint8_t *Wq, uint8_t *scale, int m, int n, void *stream)
+{
+    const teal_status st = check_mx4_layout(W_rowmajor, Wq, scale, m, n);
+    if (st != TEAL_OK) return st;
+    return from_hip(teal::launch_pack_mx4(W_rowmajor, Wq, scale, m, n, static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W_rowmajor, int m, int n, void *stream)
+{
+    const teal_status st = check_mx4_layout(W_rowmajor, Wq, scale, m, n);
+    if (st != TEAL_OK) return st;
+    return from_hip(teal::launch_unpack_mx4(Wq, scale, W_rowmajor, m, n, static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_sparse_gemv_mx4(const uint8_t *Wq, const uint8_t *scale, const void *x_f16, float t, float *y,
+                                 int m, int n, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const GemvArgs a{Wq, x_f16, t, y, m, n, workspace, workspace_bytes};
+    if (!scale) return TEAL_ERR_NULL;
+    const teal_status st = check_gemv(a, 32);
+    if (st != TEAL_OK) return st;
+    if (!aligned(scale, 16)) return TEAL_ERR_ALIGN;
+    return from_hip(teal::launch_gemv_mx4(Wq, scale, x_f16, t, y, m, n, ws_partials(workspace, m),
+                                          ws_counters(workspace), mx4_shape(m, &n, 1),
+                                          static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_sparse_gemv_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *gate, const float *up,
+                                        float t, float *y, int m, int n, void *workspace, size_t workspace_bytes,
+                                        void *stream)
+{
+    if (!up || !scale) return TEAL_ERR_NULL;
+    const GemvArgs a{Wq, gate, t, y, m, n, workspace, workspace_bytes};
+    const teal_status st = check_gemv(a, 32);
+    if (st != TEAL_OK) return st;
+    if (!aligned(gate, 4) || !aligned(up, 4) || !aligned(scale, 16)) return TEAL_ERR_ALIGN;
+    // The launch shape of teal_sparse_gemv_mx4: same sums, bit for bit.
+    return from_hip(teal::launch_gemv_mx4_swiglu(Wq, scale, gate, up, t, y, m, n, ws_partials(workspace, m),
+                                                 ws_counters(workspace), mx4_shape(m, &n, 1),
+                                                 static_cast<hipStream_t>(stream)));
+}
+
+// The checks that the grouped calls share; the input's own are the caller's.
+static teal_status check_mx4_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale, const float *t,
+                                   float *const *y, const int *n, int m, int m_most, int m_multiple, void *workspace,
+                                   size_t workspace_bytes)
+{
+    if (count < 1 || count > teal::kMaxMatrices) return TEAL_ERR_UNSUPPORTED;
+    if (!Wq || !scale || !t || !y || !n || !workspace) return TEAL_ERR_NULL;
+    long long n_total = 0;
+    for (int k = 0; k < count; ++k) {
+        if (!Wq[k] || !scale[k] || !y[k]) return TEAL_ERR_NULL;
+        if (n[k] < 32 || n[k] > teal::kMaxDim || n[k] % 32 != 0) return TEAL_ERR_SHAPE;
+        n_total += n[k];
+    }
+    if (m < m_multiple || m > m_most || m % m_multiple != 0 || n_total > teal::kMaxDim) return TEAL_ERR_SHAPE;
+    for (int k = 0; k < count; ++k)
+        if (!aligned(Wq[k], 16) || !aligned(scale[k], 16) || !aligned(y[k], 4)) return TEAL_ERR_ALIGN;
+    if (!aligned(workspace, kAlignWorkspace)) return TEAL_ERR_ALIGN;
+    for (int k = 0; k < count; ++k)
+        if (!threshold_ok(t[k])) return TEAL_ERR_THRESHOLD;
+    if (workspace_bytes < teal_workspace_bytes(m, (int)n_total)) return TEAL_ERR_WORKSPACE;
+    return TEAL_OK;
+}
+
+teal_status teal_sparse_gemv_mx4_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                       const float *t, float *const *y, const int *n, const void *x_f16, int m,
+                                       void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!x_f16) return TEAL_ERR_NULL;
+    const teal_status st = check_mx4_multi(count, Wq, scale, t, y, n, m, teal::kMaxDim, 1, workspace,
+                                           workspace_bytes);
+    if (st != TEAL_OK) return st;
+    if (!aligned(x_f16, 2)) return TEAL_ERR_ALIGN;
+    return from_hip(teal::launch_gemv_mx4_multi(count, Wq, scale, t, y, n, x_f16, m, ws_partials(workspace, m),
+                                                ws_counters(workspace), mx4_shape(m, n, count),
+                                                static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_sparse_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                               const float *t, float *const *y, const int *n, const float *h,
+                                               const float *gamma, float eps, int m, void *workspace,
+                                               size_t workspace_bytes, void *stream)
+{
+    if (!h || !gamma) return TEAL_ERR_NULL;
+    const teal_status st = check_mx4_multi(count, Wq, scale, t, y, n, m, teal::kMaxNormInput, 8, workspace,
+                                           workspace_bytes);
+    if (st != TEAL_OK) return st;
+    if (!aligned(h, 16) || !aligned(gamma, 4)) return TEAL_ERR_ALIGN;
+    if (!norm_eps_ok(eps)) return TEAL_ERR_THRESHOLD;
+    // The launch shape of teal_sparse_gemv_mx4_multi: same sums, bit for bit.
+    return from_hip(teal::launch_gemv_mx4_rmsnorm_multi(count, Wq, scale, t, y, n, h, gamma, eps, m,
+                                                        ws_partials(workspace, m), ws_counters(workspace),
+                                                        mx4_shape(m, n, count), static_cast<hipStream_t>(stream)));
+}
+
+// ---- a mixture of experts ----
+
+static_assert(TEAL_MAX_EXPERTS == teal::kMaxExperts && TEAL_MAX_TOP_K == teal::kMaxTopK &&
+                  TEAL_MAX_BATCH == teal::kMaxBatch,
+              "the limits the header states are the kernels'");
+
+teal_status teal_route_experts(const float *logits, const float *bias, int score, int tokens, int experts,
+                               int groups, int top_groups, int group_top, int top_k, int renormalise, float scaling,
+                               int32_t *idx, float *weight, void *stream)
+{
+    if (tokens < 0 || tokens > teal::kMaxDim || experts < 1 || experts > TEAL_MAX_EXPERTS) return TEAL_ERR_SHAPE;
+    if ((!logits || !idx || !weight) && tokens > 0) return TEAL_ERR_NULL;
+    if (!aligned(logits, 4) || !aligned(bias, 4) || !aligned(idx, 4) || !aligned(weight, 4)) return TEAL_ERR_ALIGN;
+    if (!std::isfinite(scaling)) return TEAL_ERR_THRESHOLD;
+    if (score != TEAL_SCORE_SOFTMAX && score != TEAL_SCORE_SIGMOID) return TEAL_ERR_UNSUPPORTED;
+    if (groups < 1 || groups > teal::kMaxExpertGroups || experts % groups != 0) return TEAL_ERR_UNSUPPORTED;
+    if (top_groups < 1 || top_groups > groups || (group_top != 1 && group_top != 2)) return TEAL_ERR_UNSUPPORTED;
+    if (top_k < 1 || top_k > TEAL_MAX_TOP_K || top_k > experts / groups * top_groups) return TEAL_ERR_UNSUPPORTED;
+    if (tokens == 0) return TEAL_OK;
+    const teal::RouteHostArgs h{logits,     bias,      score == TEAL_SCORE_SIGMOID, renormalise != 0, tokens, experts,
+                                groups,     top_groups, group_top,                  top_k,            scaling, idx,
+                                weight};
+    return from_hip(teal::launch_route_experts(h, static_cast<hipStream_t>(stream)));
+}
+
+size_t teal_workspace_bytes_experts(int m, int n, int pairs)
+{
+    if (m < 1 || m > teal::kMaxDim || n < 1 || pairs < 1 || pairs > TEAL_MAX_BATCH * TEAL_MAX_TOP_K ||
+        (long long)n * pairs > teal::kMaxDim)
+        return 0;
+    const size_t bytes = teal::kCounterBytes + report_bytes(m) +
+                         experts_partial_floats(m, (long long)n * pairs) * sizeof(float);
+    return (bytes + kAlignWorkspace - 1) / kAlignWorkspace * kAlignWorkspace;
+}
+
+// The checks and the launch of the four calls; h has the input that the call takes (x, or weight, gate and up).
+static teal_status experts_call(int bits, teal::ExpertHostArgs h, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int multiple = bits == 16 ? 8 : 32;
+    const bool down = h.x_f16 == nullptr;
+    if (h.count < 1 || h.count > teal::kMaxMatrices) return TEAL_ERR_UNSUPPORTED;
+    if (!h.W || (bits == 4 && !h.scale) || !h.t || !h.y || !h.n || !h.idx || !workspace) return TEAL_ERR_NULL;
+    if (down && (!h.weight || !h.gate || !h.up)) return TEAL_ERR_NULL;
+    long long n_total = 0;
+    for (int k = 0; k < h.count; ++k) {
+        if (!h.W[k] || (bits == 4 && !h.scale[k]) || !h.t[k] || !h.y[k]) return TEAL_ERR_NULL;
+        if (h.n[k] < multiple || h.n[k] > teal::kMaxDim || h.n[k] % multiple != 0) return TEAL_ERR_SHAPE;
+        n_total += h.n[k];
+    }
+    if (h.m < 1 || h.m > teal::kMaxDim || h.tokens < 1 || h.tokens > TEAL_MAX_BATCH || h.top_k < 1 ||
+        h.top_k > TEAL_MAX_TOP_K || h.experts < 1 || h.experts > TEAL_MAX_EXPERTS)
+        return TEAL_ERR_SHAPE;
+    const int pairs = h.tokens * h.top_k;
+    if (n_total * pairs > teal::kMaxDim) return TEAL_ERR_SHAPE;
+    for (int k = 0; k < h.count; ++k)
+        if (!aligned(h.W[k], 16) || (bits == 4 && !aligned(h.scale[k], 16)) || !aligned(h.t[k], 4) ||
+            !aligned(h.y[k], 4))
+            return TEAL_ERR_ALIGN;
+    if (!aligned(h.idx, 4) || !aligned(h.x_f16, 2) || !aligned(h.weight, 4) || !aligned(h.gate, 4) ||
+        !aligned(h.up, 4) || !aligned(workspace, kAlignWorkspace))
+        return TEAL_ERR_ALIGN;
+    if (workspace_bytes < teal_workspace_bytes_experts(h.m, (int)n_total, pairs)) return TEAL_ERR_WORKSPACE;
+    h.partial = ws_partials(workspace, h.m);
+    h.counters = ws_counters(workspace);
+    const int joined = down ? h.top_k : 1;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (bits == 16)
+        return from_hip(teal::launch_experts_bf16(h, experts_shape(pairs, h.m, h.n, h.count, joined, 8, 128, 64, 64), st));
+    return from_hip(teal::launch_experts_mx4(h, experts_shape(pairs, h.m, h.n, h.count, joined, 32, 256, 128, 16), st));
+}
+
+static teal::ExpertHostArgs experts_args(int count, const void *const *W, const void *const *scale,
+                                         const float *const *t, float *const *y, const int *n, int experts,
+                                         const int32_t *idx, int tokens, int top_k, int m)
+{
+    teal::ExpertHostArgs h{};
+    h.count = count;
+    h.W = W;
+    h.scale = scale;
+    h.t = t;
+    h.y = y;
+    h.n = n;
+    h.experts = experts;
+    h.tokens = tokens;
+    h.top_k = top_k;
+    h.idx = idx;
+    h.m = m;
+    return h;
+}
+
+teal_status teal_sparse_experts_bf16(int count, const void *const *Wt_bf16, const float *const *t, float *const *y,
+                                     const int *n, int experts, const int32_t *idx, int tokens, int top_k,
+                                     const void *X_f16, int m, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X_f16) return TEAL_ERR_NULL;
+    teal::ExpertHostArgs h = experts_args(count, Wt_bf16, nullptr, t, y, n, experts, idx, tokens, top_k, m);
+    h.x_f16 = X_f16;
+    return experts_call(16, h, workspace, workspace_bytes, stream);
+}
+
+teal_status teal_sparse_experts_mx4(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                    const float *const *t, float *const *y, const int *n, int experts,
+                                    const int32_t *idx, int tokens, int top_k, const void *X_f16, int m,
+                                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X_f16) return TEAL_ERR_NULL;
+    teal::ExpertHostArgs h = experts_args(count, reinterpret_cast<const void *const *>(Wq),
+                                          reinterpret_cast<const void *const *>(scale), t, y, n, experts, idx, tokens,
+                                          top_k, m);
+    h.x_f16 = X_f16;
+    return experts_call(4, h, workspace, workspace_bytes, stream);
+}
+
+teal_status teal_sparse_experts_bf16_swiglu(const void *Wt_bf16, const float *t, float *y, int experts,
+                                            const int32_t *idx, const float *weight, int tokens, int top_k,
+                                            const float *gate, const float *up, int m, int n, void *workspace,
+                                            size_t workspace_bytes, void *stream)
+{
+    teal::ExpertHostArgs h = experts_args(1, &Wt_bf16, nullptr, &t, &y, &n, experts, idx, tokens, top_k, m);
+    h.weight = weight;
+    h.gate = gate;
+    h.up = up;
+    return experts_call(16, h, workspace, workspace_bytes, stream);
+}
+
+teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *t, float *y,
+                                           int experts, const int32_t *idx, const float *weight, int tokens,
+                                           int top_k, const float *gate, const float *up, int m, int n,
+                                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    const void *W = Wq, *sc = scale;
+    teal::ExpertHostArgs h = experts_args(1, &W, &sc, &t, &y, &n, experts, idx, tokens, top_k, m);
+    h.weight = weight;
+    h.gate = gate;
+    h.up = up;
+    return experts_call(4, h, workspace, workspace_bytes, stream);
 }
 
 teal_status teal_stream_read_probe(const void *buf, size_t bytes, int blocks, uint32_t match,

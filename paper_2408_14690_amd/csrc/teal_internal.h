@@ -144,6 +144,63 @@ hipError_t launch_gemv_w4_multi(int count, const uint8_t *const *Wq, const void 
                                 int m, float *partial, int *counters, const GemvShape &shape,
                                 hipStream_t stream);
 
+// Microscaled 4-bit weights: [m][n / 2] bytes of codes, a scale byte per channel and block of 32 outputs in tiles
+// of 8 channels by 16 blocks (gemv_mx4.hip).  Shapes with 16 lanes per row, 8 wavefronts, 4 loads per batch.
+constexpr int kMx4TileBytes = 128;
+__host__ __device__ constexpr int mx4_scale_tiles(int n) { return (n + 511) / 512; }
+__host__ __device__ constexpr size_t mx4_scale_bytes(int m, int n)
+{
+    return (size_t)((m + 7) / 8) * mx4_scale_tiles(n) * kMx4TileBytes;
+}
+hipError_t launch_pack_mx4(const void *W_rowmajor, uint8_t *Wq, uint8_t *scale, int m, int n, hipStream_t stream);
+hipError_t launch_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W_rowmajor, int m, int n,
+                             hipStream_t stream);
+hipError_t launch_gemv_mx4(const uint8_t *Wq, const uint8_t *scale, const void *x_f16, float t, float *y, int m,
+                           int n, float *partial, int *counters, const GemvShape &shape, hipStream_t stream);
+hipError_t launch_gemv_mx4_swiglu(const uint8_t *Wq, const uint8_t *scale, const float *gate, const float *up,
+                                  float t, float *y, int m, int n, float *partial, int *counters,
+                                  const GemvShape &shape, hipStream_t stream);
+hipError_t launch_gemv_mx4_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale, const float *t,
+                                 float *const *y, const int *n, const void *x_f16, int m, float *partial,
+                                 int *counters, const GemvShape &shape, hipStream_t stream);
+hipError_t launch_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *Wq, const uint8_t *const *scale,
+                                         const float *t, float *const *y, const int *n, const float *h,
+                                         const float *gamma, float eps, int m, float *partial, int *counters,
+                                         const GemvShape &shape, hipStream_t stream);
+
+// The experts a router chose, for a small batch of tokens (gemv_experts.h).  With `weight` the W_down step of the
+// experts (gate and up in, one matrix, y[tokens][n]), else count matrices on x (y_k[tokens][top_k][n_k]).
+struct ExpertHostArgs {
+    int count;
+    const void *const *W;          // of expert 0 each
+    const void *const *scale;      // microscaled weights, else NULL
+    const float *const *t;         // device arrays [experts]
+    float *const *y;
+    const int *n;
+    int experts, tokens, top_k;
+    const int *idx;                // device, [tokens][top_k]
+    const void *x_f16;
+    const float *weight, *gate, *up;
+    int m;
+    float *partial;
+    int *counters;
+};
+hipError_t launch_experts_bf16(const ExpertHostArgs &h, const GemvShape &sh, hipStream_t stream);
+hipError_t launch_experts_mx4(const ExpertHostArgs &h, const GemvShape &sh, hipStream_t stream);
+
+constexpr int kMaxExperts = 1024;      // of a router
+constexpr int kMaxExpertGroups = 64;
+constexpr int kMaxTopK = 32;           // experts per token
+struct RouteHostArgs {
+    const float *logits, *bias;
+    bool sigmoid, renormalise;
+    int tokens, experts, groups, top_groups, group_top, top_k;
+    float scaling;
+    int *idx;
+    float *weight;
+};
+hipError_t launch_route_experts(const RouteHostArgs &h, hipStream_t stream);
+
 // The MLP of a block in one launch (Appendix A.3): gate and up from x, then W_down on
 // SiLU(gate) . up, the blocks of W_down waiting for the gate / up tiles they read.
 struct MlpLaunch {

@@ -293,3 +293,61 @@ def layer_inputs(model: str, layer: int = 0):
         w = weights_bf16(n, m, weight_seed(cfg, layer, proj))
         x = make_x(m, x_seed(cfg, layer, proj), PROJ_DIST[proj])
         yield proj, n, m, w, x
+
+
+# ----------------------------------------------------------------------------
+# microscaled 4-bit weights
+# ----------------------------------------------------------------------------
+
+MX4_LEVELS = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx4_scale_places(m: int, n: int) -> np.ndarray:
+    """Place of the scale byte of channel i and block b in the stored scales, [m][n / 32]."""
+    i, b = np.arange(m)[:, None], np.arange(n // 32)[None, :]
+    return (i // 8 * -(-n // 512) + b // 16) * 128 + i % 8 * 16 + b % 16
+
+
+def mx4_scale_bytes(m: int, n: int) -> int:
+    return -(-m // 8) * -(-n // 512) * 128
+
+
+def quantize_mx4(w_bits: np.ndarray):
+    """Canonical W[n][m] as bf16 bit patterns -> (codes [m][n/2], scales as stored).
+
+    Per channel and block of 32 outputs: X = 2^(floor(log2 largest) - 2), at least 2^-127, and each weight to the nearest
+    level (ties to the even code, beyond the last to the last) with its sign."""
+    n, m = w_bits.shape
+    w = bf16_bits_to_f32(w_bits).astype(np.float64).T.reshape(m, n // 32, 32)
+    largest = np.abs(w).max(-1)                           # a NaN stays one
+    finite = np.isfinite(largest)
+    # frexp: largest = f * 2^e with f in [0.5, 1)
+    exponent = np.frexp(np.where(finite & (largest > 0), largest, 1.0))[1] - 1
+    scale = np.where(largest > 0, np.maximum(exponent - 2 + 127, 0), 0)
+    scale = np.where(finite, scale, 255).astype(np.uint8)
+    ratio = np.abs(w) * 2.0 ** (127.0 - scale[..., None])
+    ratio = np.where(finite[..., None], ratio, 0.0)
+    order = np.array([0, 2, 4, 6, 1, 3, 5, 7])            # even codes first: a tie takes the first of the nearest
+    code = order[np.abs(ratio[..., None] - MX4_LEVELS[order]).argmin(-1)]
+    code = np.where(finite[..., None], code | np.signbit(w).astype(np.int64) << 3, 0)
+    code = code.reshape(m, n).astype(np.uint8)
+    stored = np.zeros(mx4_scale_bytes(m, n), np.uint8)
+    stored[mx4_scale_places(m, n)] = scale
+    return code[:, 0::2] | code[:, 1::2] << 4, stored
+
+
+def mx4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """The weights W[m][n] (input channel first) that codes and scales stand for, fp64."""
+    m, n = codes.shape[0], 2 * codes.shape[1]
+    code = np.stack((codes & 15, codes >> 4), -1).reshape(m, n)
+    scale = scales[mx4_scale_places(m, n)].repeat(32, -1)
+    value = MX4_LEVELS[code & 7] * np.where(code & 8, -1.0, 1.0) * 2.0 ** (scale.astype(np.float64) - 127)
+    return np.where(scale == 255, np.nan, value)
+
+
+def random_mx4(m: int, n: int, seed: int):
+    """Random codes and scales of weights of about 0.02: (codes [m][n/2], scales as stored)."""
+    rng = _rng(seed)
+    stored = np.zeros(mx4_scale_bytes(m, n), np.uint8)
+    stored[mx4_scale_places(m, n)] = rng.integers(117, 123, (m, n // 32))
+    return rng.integers(0, 256, (m, n // 2), dtype=np.uint8), stored
