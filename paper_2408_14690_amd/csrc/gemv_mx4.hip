@@ -14,6 +14,8 @@
 
 namespace teal {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 struct FmtMx4 {
     static constexpr int kElemsPerLane = 32;   // 16 bytes = 32 codes, one block
     static constexpr int kBitsPerElem = 4;
@@ -339,92 +341,140 @@ hipError_t launch_experts_mx4(const ExpertHostArgs &h, const GemvShape &sh, hipS
 }
 
 // ---- the format itself: bf16 weights in and out ----
+//
+// A thread block has 128 channels by 128 outputs, a wavefront one block of 32 outputs of all of them, a lane two
+// neighbouring channels: the 32 rows of W[n][m] are read (written) 256 bytes at a time, a block's 32 weights are in
+// one lane's registers, and the conversions of the hardware take and give two outputs at once.  Codes and scales
+// pass through LDS so that a channel's 64 bytes of codes and 4 scales travel together: 16 bytes and one byte per
+// lane and wavefront were four times the requests.
+constexpr int kMx4PackRows = 128, kMx4PackWaves = 4;
 
-// One thread block lays out 64 channels by 256 outputs: the weights of an output are contiguous along the
-// channels, the codes of a channel along the outputs, so they are turned through LDS.  A thread then has one block
-// of 32 outputs of one channel in two pieces of 16.
-constexpr int kMx4PackRows = 64, kMx4PackCols = 256;
+// Two bf16 values of neighbouring channels; a row of W begins on an even address only.
+struct __attribute__((packed, aligned(2))) Mx4Pair {
+    unsigned v;
+};
 
-__device__ __forceinline__ unsigned mx4_code(float a, unsigned sign)
+struct Mx4PackTile {
+    u32x4 codes[kMx4PackRows][kMx4PackWaves + 1];     // one of padding: lanes two channels apart do not meet in a bank
+    unsigned char scale[kMx4PackRows][kMx4PackWaves];
+};
+
+// Codes of channels c and c + 64 of the tile, all four blocks: where thread `t` has its part of the LDS tile and of
+// memory, for pass k of 2.
+__device__ __forceinline__ int mx4_tile_channel(int t, int k) { return k * 64 + t / kMx4PackWaves; }
+
+__device__ __forceinline__ size_t mx4_scale_place(int i, int b, int n)
 {
-    // nearest level, ties to the even code; a is at most 8
-    const unsigned c = (unsigned)(a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) +
-                       (a > 5.f);
-    return c | sign << 3;
+    return ((size_t)(i / 8) * mx4_scale_tiles(n) + b / 16) * kMx4TileBytes + i % 8 * 16 + b % 16;
 }
 
-__global__ __launch_bounds__(256) void pack_mx4_kernel(const uint16_t *__restrict__ W, uint8_t *__restrict__ Wq,
-                                                       uint8_t *__restrict__ scale, int m, int n, int tiles_m)
+__global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint16_t *__restrict__ W,
+                                                                      uint8_t *__restrict__ Wq,
+                                                                      uint8_t *__restrict__ scale, int m, int n,
+                                                                      int tiles_m)
 {
-    __shared__ uint16_t tile[kMx4PackCols][kMx4PackRows + 2];
-    const int i0 = (int)(blockIdx.x % tiles_m) * kMx4PackRows;
-    const int j0 = (int)(blockIdx.x / tiles_m) * kMx4PackCols;
-    const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
-    for (int r = r0; r < kMx4PackCols; r += 4) {
-        const int j = j0 + r, i = i0 + c;
-        tile[r][c] = j < n && i < m ? W[(size_t)j * m + i] : 0;
-    }
-    __syncthreads();
-    for (int b = r0; b < kMx4PackCols / 32; b += 4) {       // channel i0 + c, block b of the tile
-        const int i = i0 + c, j = j0 + 32 * b;
-        if (j >= n) break;
-        unsigned largest = 0;
-        for (int k = 0; k < 32; ++k) largest = max(largest, (unsigned)tile[32 * b + k][c] & 0x7FFFu);
-        // floor(log2) of the largest magnitude, of subnormal ones by their leading bit
-        int e;
-        if (largest >= 0x80u) e = (int)(largest >> 7) - 127;
-        else e = 31 - __clz((int)max(largest, 1u)) - 133;
-        const bool finite = largest < 0x7F80u;
-        const int s = finite ? max(e - 2 + 127, 0) : 255;
-        u32x4 codes = {0u, 0u, 0u, 0u};
-        if (finite) {
-            for (int k = 0; k < 32; ++k) {
-                const unsigned h = tile[32 * b + k][c];
-                const float a = ldexpf(__uint_as_float((h & 0x7FFFu) << 16), 127 - s);
-                codes[k / 8] |= mx4_code(a, h >> 15) << 4 * (k % 8);
+    __shared__ Mx4PackTile tile;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i0 = blockIdx.x % tiles_m * kMx4PackRows, b0 = blockIdx.x / tiles_m * kMx4PackWaves;
+    const int i = i0 + 2 * lane, blocks = n / 32;
+    if (b0 + w < blocks) {                                  // wavefront-uniform
+        unsigned v[32];                                     // channel i in the lower half, i + 1 in the upper
+        const uint16_t *first = W + (size_t)(b0 + w) * 32 * m;
+        if (i0 + kMx4PackRows <= m) {
+#pragma unroll
+            for (int r = 0; r < 32; ++r) v[r] = reinterpret_cast<const Mx4Pair *>(first + (size_t)r * m + i)->v;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 32; ++r) {
+                const uint16_t *p = first + (size_t)r * m + i;
+                v[r] = i + 1 < m ? reinterpret_cast<const Mx4Pair *>(p)->v : i < m ? *p : 0u;
             }
         }
-        if (i < m) *reinterpret_cast<u32x4 *>(Wq + (size_t)i * (n / 2) + j / 2) = codes;
-        // past the last channel of a tile of scales: zeros
-        if (i < (m + 7) / 8 * 8)
-            scale[((size_t)(i / 8) * mx4_scale_tiles(n) + j / 512) * kMx4TileBytes + i % 8 * 16 + j / 32 % 16] =
-                i < m ? (uint8_t)s : 0;
-    }
-    // past the last block of a tile of scales
-    if (j0 + kMx4PackCols >= n) {
-        const int blocks = n / 32, end = (blocks + 15) / 16 * 16;
-        for (int b = blocks + r0; b < end; b += 4) {
-            const int i = i0 + c;
-            if (i < (m + 7) / 8 * 8)
-                scale[((size_t)(i / 8) * mx4_scale_tiles(n) + b / 16) * kMx4TileBytes + i % 8 * 16 + b % 16] = 0;
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 largest = {0, 0};
+#pragma unroll
+        for (int r = 0; r < 32; ++r)
+            largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, v[r] & 0x7FFF7FFFu));
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            // floor(log2) of the largest magnitude; below 2^-125 the scale is the smallest one anyway
+            const int s = largest[c] >= 0x7F80u ? 255 : max((int)(largest[c] >> 7) - 2, 0);
+            const float x = __uint_as_float((unsigned)s << 23);
+            u32x4 codes = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                unsigned word = 0;
+#define TEAL_PAIR(B)                                                                           \
+    do {                                                                                       \
+        const unsigned two = __builtin_amdgcn_perm(v[8 * q + 2 * B + 1], v[8 * q + 2 * B],     \
+                                                   c ? 0x07060302u : 0x05040100u);             \
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, __builtin_bit_cast(bf16x2, two), x, B); \
+    } while (0)
+                TEAL_PAIR(0);
+                TEAL_PAIR(1);
+                TEAL_PAIR(2);
+                TEAL_PAIR(3);
+#undef TEAL_PAIR
+                codes[q] = s == 255 ? 0u : word;
+            }
+            tile.codes[2 * lane + c][w] = codes;
+            tile.scale[2 * lane + c][w] = i + c < m ? (unsigned char)s : 0;
         }
+    } else {
+        tile.scale[2 * lane][w] = 0;
+        tile.scale[2 * lane + 1][w] = 0;
     }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = mx4_tile_channel(threadIdx.x, k), b = b0 + (int)threadIdx.x % kMx4PackWaves;
+        if (i0 + c < m && b < blocks)
+            *reinterpret_cast<u32x4 *>(Wq + ((size_t)(i0 + c) * blocks + b) * 16) =
+                tile.codes[c][threadIdx.x % kMx4PackWaves];
+    }
+    // zeros past the last channel and block of a tile of scales
+    const int c = threadIdx.x;
+    if (c < kMx4PackRows && i0 + c < (m + 7) / 8 * 8)
+        for (int b = b0; b < (b0 + kMx4PackWaves < blocks ? b0 + kMx4PackWaves : mx4_scale_tiles(n) * 16);
+             b += kMx4PackWaves)
+            *reinterpret_cast<unsigned *>(scale + mx4_scale_place(i0 + c, b, n)) =
+                b == b0 ? *reinterpret_cast<const unsigned *>(tile.scale[c]) : 0u;
 }
 
-__global__ __launch_bounds__(256) void unpack_mx4_kernel(const uint8_t *__restrict__ Wq,
-                                                         const uint8_t *__restrict__ scale, uint16_t *__restrict__ W,
-                                                         int m, int n, int tiles_m)
+__global__ __launch_bounds__(kMx4PackWaves * 64) void unpack_mx4_kernel(const uint8_t *__restrict__ Wq,
+                                                                        const uint8_t *__restrict__ scale,
+                                                                        uint16_t *__restrict__ W, int m, int n,
+                                                                        int tiles_m)
 {
-    __shared__ uint16_t tile[kMx4PackCols][kMx4PackRows + 2];
-    const int i0 = (int)(blockIdx.x % tiles_m) * kMx4PackRows;
-    const int j0 = (int)(blockIdx.x / tiles_m) * kMx4PackCols;
-    const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
-    for (int b = r0; b < kMx4PackCols / 32; b += 4) {
-        const int i = i0 + c, j = j0 + 32 * b;
-        if (j >= n || i >= m) break;
-        const u32x4 codes = *reinterpret_cast<const u32x4 *>(Wq + (size_t)i * (n / 2) + j / 2);
-        const unsigned s = scale[((size_t)(i / 8) * mx4_scale_tiles(n) + j / 512) * kMx4TileBytes + i % 8 * 16 +
-                                 j / 32 % 16];
-        const float x = __uint_as_float(s << 23);
+    __shared__ Mx4PackTile tile;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i0 = blockIdx.x % tiles_m * kMx4PackRows, b0 = blockIdx.x / tiles_m * kMx4PackWaves;
+    const int blocks = n / 32;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = mx4_tile_channel(threadIdx.x, k), b = b0 + (int)threadIdx.x % kMx4PackWaves;
+        if (i0 + c < m && b < blocks)
+            tile.codes[c][threadIdx.x % kMx4PackWaves] =
+                *reinterpret_cast<const u32x4 *>(Wq + ((size_t)(i0 + c) * blocks + b) * 16);
+    }
+    if (threadIdx.x < kMx4PackRows && i0 + (int)threadIdx.x < m)
+        *reinterpret_cast<unsigned *>(tile.scale[threadIdx.x]) =
+            *reinterpret_cast<const unsigned *>(scale + mx4_scale_place(i0 + (int)threadIdx.x, b0, n));
+    __syncthreads();
+    if (b0 + w >= blocks) return;
+    const int i = i0 + 2 * lane;
+    if (i >= m) return;
+    // two outputs of one channel each, by channel
+    unsigned two[2][16];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const u32x4 codes = tile.codes[2 * lane + c][w];
+        const float x = __uint_as_float((unsigned)tile.scale[2 * lane + c][w] << 23);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
 #define TEAL_PAIR(B)                                                                           \
-    do {                                                                                       \
-        const unsigned w = __builtin_bit_cast(                                                 \
-            unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], x, B));              \
-        tile[32 * b + 8 * q + 2 * B][c] = (uint16_t)w;                                         \
-        tile[32 * b + 8 * q + 2 * B + 1][c] = (uint16_t)(w >> 16);                             \
-    } while (0)
+    two[c][4 * q + B] =                                                                        \
+        __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], x, B))
             TEAL_PAIR(0);
             TEAL_PAIR(1);
             TEAL_PAIR(2);
@@ -432,28 +482,42 @@ __global__ __launch_bounds__(256) void unpack_mx4_kernel(const uint8_t *__restri
 #undef TEAL_PAIR
         }
     }
-    __syncthreads();
-    for (int r = r0; r < kMx4PackCols; r += 4) {
-        const int j = j0 + r, i = i0 + c;
-        if (j < n && i < m) W[(size_t)j * m + i] = tile[r][c];
+    uint16_t *first = W + (size_t)(b0 + w) * 32 * m + i;
+    const bool both = i + 1 < m;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) {
+        const unsigned v = __builtin_amdgcn_perm(two[1][r / 2], two[0][r / 2], r % 2 ? 0x07060302u : 0x05040100u);
+        if (both) reinterpret_cast<Mx4Pair *>(first + (size_t)r * m)->v = v;
+        else first[(size_t)r * m] = (uint16_t)v;
     }
 }
 
+// Tiles of the channels, fastest in the grid, and all tiles.
+struct Mx4LayoutGrid {
+    int tiles_m;
+    long long tiles;
+    Mx4LayoutGrid(int m, int n)
+        : tiles_m((m + kMx4PackRows - 1) / kMx4PackRows),
+          tiles((long long)tiles_m * ((n / 32 + kMx4PackWaves - 1) / kMx4PackWaves))
+    {
+    }
+};
+
 hipError_t launch_pack_mx4(const void *W, uint8_t *Wq, uint8_t *scale, int m, int n, hipStream_t stream)
 {
-    const long long tiles_m = (m + kMx4PackRows - 1) / kMx4PackRows, tiles_n = (n + kMx4PackCols - 1) / kMx4PackCols;
-    if (tiles_m * tiles_n > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(pack_mx4_kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, stream,
-                       static_cast<const uint16_t *>(W), Wq, scale, m, n, (int)tiles_m);
+    const Mx4LayoutGrid g(m, n);
+    if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;      // more weights than a GPU has bytes
+    hipLaunchKernelGGL(pack_mx4_kernel, dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream,
+                       static_cast<const uint16_t *>(W), Wq, scale, m, n, g.tiles_m);
     return hipGetLastError();
 }
 
 hipError_t launch_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W, int m, int n, hipStream_t stream)
 {
-    const long long tiles_m = (m + kMx4PackRows - 1) / kMx4PackRows, tiles_n = (n + kMx4PackCols - 1) / kMx4PackCols;
-    if (tiles_m * tiles_n > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(unpack_mx4_kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, stream, Wq, scale,
-                       static_cast<uint16_t *>(W), m, n, (int)tiles_m);
+    const Mx4LayoutGrid g(m, n);
+    if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(unpack_mx4_kernel, dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream, Wq, scale,
+                       static_cast<uint16_t *>(W), m, n, g.tiles_m);
     return hipGetLastError();
 }
 
