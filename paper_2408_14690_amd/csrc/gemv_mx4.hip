@@ -43,37 +43,41 @@ struct FmtMx4 {
     struct ColumnScale {};
     static __device__ __forceinline__ ColumnScale column_scale(const Args &, int) { return {}; }
     static __device__ __forceinline__ float finish(float sum, ColumnScale) { return sum; }
-
-    // The conversion scales by the exponent of an fp32 number: exact, and NaN for the scale byte 255.
-    static __device__ __forceinline__ void fma(float (&acc)[32], u32x4 v, unsigned scale, float xv)
-    {
-        const float sc = __uint_as_float(scale << 23);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-#define TEAL_PAIR(B)                                                                           \
-    do {                                                                                       \
-        const auto w = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[q], sc, B);                  \
-        acc[8 * q + 2 * B] = fmaf(xv, w[0], acc[8 * q + 2 * B]);                               \
-        acc[8 * q + 2 * B + 1] = fmaf(xv, w[1], acc[8 * q + 2 * B + 1]);                       \
-    } while (0)
-            TEAL_PAIR(0);
-            TEAL_PAIR(1);
-            TEAL_PAIR(2);
-            TEAL_PAIR(3);
-#undef TEAL_PAIR
-        }
-    }
 };
 
 constexpr int kMx4Waves = 8;
 constexpr int kMx4Unroll = 4;
 constexpr int kMx4Lanes = 16;
 
+// The products run on the matrix cores.  v_mfma_f32_16x16x32_bf16: a lane's 8 values of A are 8 of the 32 places of
+// the sum, its lane % 16 the row, lane / 16 the quarter.  A lane's 16 bytes are one block: 4 instructions per word
+// turn its 8 codes into 8 bf16 numbers, exact and already scaled by the block's power of two, and they go in as
+// they come, 16 blocks (rows of A) by 4 channels (quarters).  B separates the columns again: it is zero except
+// where the place in the word equals the column, B[8 g + j][j] = the activation of quarter g's channel.  Columns j and
+// j + 8 of B take two parts of it: an fp16 number has 11 significant bits, 8 of them in the first bf16 number and
+// the rest in the second, so the products are exact; they are added in fp32, four channels at a time (against
+// binary64 as near as a chain of FMAs, for sizes 2^24 apart too).  Of the instruction for 4-bit floats
+// itself, which would need no conversion, the sums lose bits: products far below the largest one of an
+// instruction are cut to 17 bits or so, 5e-5 of the result where 2e-7 is what fp32 gives.
+struct Bf16Parts {
+    static constexpr bool kMagnitude = false;
+    // Channel of the slice, and the two parts of x; of an infinity the second is zero.
+    static __device__ __forceinline__ int2 entry(int, int offset, float x)
+    {
+        const unsigned first = __float_as_uint(x) & 0xFFFF0000u;
+        const float rest = x == __uint_as_float(first) ? 0.f : x - __uint_as_float(first);
+        return make_int2(offset, (int)__builtin_amdgcn_perm(__float_as_uint(rest), first, 0x07060302u));
+    }
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
 template <int U>
 struct Mx4Batch {
     u32x4 v[U];
     unsigned sc[U];
-    float xv[U];
+    unsigned x[U];
 };
 
 // Work of one block: output tile `tile` (tile_cols columns, at most 512) x K-slice `s` (ks channels).  16 lanes share a
@@ -87,14 +91,15 @@ __device__ __forceinline__ int mx4_block(const FmtMx4::Args &a, const XS &x, flo
 {
     using F = FmtMx4;
     constexpr int EPL = F::kElemsPerLane;
-    constexpr int R = 64 / LPR;
+    static_assert(LPR == 16, "the rows of the matrix instruction");
+    constexpr int R = 4;                          // rows per wavefront load
     extern __shared__ __align__(16) unsigned char smem[];
     int2 *list = reinterpret_cast<int2 *>(smem);
     float *red = reinterpret_cast<float *>(smem + (size_t)ks * sizeof(int2));
     __shared__ int counts[kCompactInts];
 
     asm volatile("" ::"s"(a.W), "s"(a.scale), "s"(partial), "s"(meet.counters), "s"(y));   // as in gemv_block
-    const int k0 = s * ks;
+    const int k0 = s * ks;                       // a multiple of 64, so of the 8 channels of a tile of scales
     const int k1 = min(m, k0 + ks);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int group_excl;
@@ -102,28 +107,41 @@ __device__ __forceinline__ int mx4_block(const FmtMx4::Args &a, const XS &x, flo
     bool compacted = false;
     if constexpr (XS::kPlainHalf) {
         if (k1 - k0 <= kPrivateSlice) {         // block-uniform: short slices need no barrier
-            cnt = compact_slice_private(x.x, t, k0, k1, w, WAVES, list, group_excl);
+            cnt = compact_slice_private<Bf16Parts>(x.x, t, k0, k1, w, WAVES, list, group_excl);
             compacted = true;
         }
     }
-    if (!compacted) cnt = compact_slice<WAVES>(x, t, k0, k1, list, counts, group_excl);
+    if (!compacted) cnt = compact_slice<WAVES, XS, Bf16Parts>(x, t, k0, k1, list, counts, group_excl);
 
     trace_mark(2);
     if constexpr (Report::kOn) {
         if (tile == 0 && !meet.word_step && threadIdx.x == (WAVES - 1) * 64) report_slice(report, s, splits, cnt);
     }
     const int lane = threadIdx.x & 63;
-    const int g = lane / LPR;
+    const int l = lane & 15, g = lane >> 4;
     const int col0 = tile * tile_cols;
-    const int col = lane_column<EPL>(col0, tile_cols, n, lane % LPR);
-    const unsigned row_bytes = (unsigned)(n / 2);
-    const unsigned char *lane_base = static_cast<const unsigned char *>(a.W) + col / 2;
-    const unsigned tiles_bytes = (unsigned)mx4_scale_tiles(n) * kMx4TileBytes;      // of 8 channels' scales
-    const unsigned char *scale_base = a.scale + (col / 512) * kMx4TileBytes + col / 32 % 16;
-
-    float acc[EPL];
+    const int col = lane_column<EPL>(col0, tile_cols, n, l);
+    // A channel's codes in units of 16 bytes, 8 channels' scales in bytes: with the channel of a slice both are products
+    // of less than 24 bits each, below 2^32 (n below 2^24, slices of at most 4096 channels).
+    static_assert(kMaxSlice <= 4096, "offsets inside a slice fit 32 bits");
+    const unsigned row_units = (unsigned)(n / 32);
+    const unsigned tiles_bytes = (unsigned)mx4_scale_tiles(n) * kMx4TileBytes;
+    const unsigned char *lane_base =
+        static_cast<const unsigned char *>(a.W) + (size_t)k0 * (unsigned)(n / 2) + col / 2;
+    const unsigned char *scale_base =
+        a.scale + (size_t)(k0 / 8) * tiles_bytes + col / 512 * kMx4TileBytes + col / 32 % 16;
+    // B: this lane's column takes place l % 8 of a word's 8, the first (l < 8) or second part of the activation
+    unsigned pick[4];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+    for (int q = 0; q < 4; ++q) {
+        const unsigned part = l < 8 ? 0x0100u : 0x0302u;
+        pick[q] = l % 8 / 2 != q ? 0x0C0C0C0Cu : l % 2 ? part << 16 | 0x0C0Cu : 0x0C0C0000u | part;
+    }
+
+    f32x4 acc[4];                                 // [word]: blocks 4 g + r, output 8 * word + l % 8, part l / 8
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    cnt = __builtin_amdgcn_readfirstlane(cnt);
     int start, mine;
     wave_share(cnt, w, WAVES, start, mine);
     if (mine > 0) {
@@ -136,14 +154,29 @@ __device__ __forceinline__ int mx4_block(const FmtMx4::Args &a, const XS &x, flo
                 const int e = (batch * U + u) * R + g;
                 const int2 ent = list[start + min(e, last)];
                 const unsigned i = (unsigned)ent.x;
-                b.xv[u] = e <= last ? __int_as_float(ent.y) : 0.f;
-                b.v[u] = load_stream16(lane_base + (size_t)i * row_bytes);
-                b.sc[u] = scale_base[(size_t)(i / 8) * tiles_bytes + i % 8 * 16];
+                b.x[u] = e <= last ? (unsigned)ent.y : 0u;
+                b.v[u] = load_stream16(lane_base + ((size_t)__umul24(i, row_units) << 4));
+                b.sc[u] = scale_base[__umul24(i >> 3, tiles_bytes) + (i << 4 & 0x70u)];
             }
         };
         auto consume = [&](const Mx4Batch<U> &b) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) F::fma(acc, b.v[u], b.sc[u], b.xv[u]);
+            for (int u = 0; u < U; ++u) {
+                const float sc = __uint_as_float(b.sc[u] << 23);
+                u32x4 B;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) B[q] = __builtin_amdgcn_perm(b.x[u], b.x[u], pick[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u32x4 A;
+                    A[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[u][q], sc, 0));
+                    A[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[u][q], sc, 1));
+                    A[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[u][q], sc, 2));
+                    A[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[u][q], sc, 3));
+                    acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, A),
+                                                                     __builtin_bit_cast(bf16x8, B), acc[q], 0, 0, 0);
+                }
+            }
         };
         Mx4Batch<U> b0, b1;
         issue(b0, 0);
@@ -164,7 +197,18 @@ __device__ __forceinline__ int mx4_block(const FmtMx4::Args &a, const XS &x, flo
     }
     trace_mark(3);
     trace_mark_thread(1, (WAVES - 1) * 64);
-    store_wave_sums<LPR>(acc, red + w * combine_row<EPL, LPR>);
+    // The lanes l < 8 take the first two words of a block and give the other two to the lane 8 further, which holds
+    // the other part.
+    float *row = red + w * combine_row<EPL, LPR> + (l < 8 ? 0 : 16) + l % 8;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float own = l < 8 ? acc[q][r] : acc[q + 2][r], give = l < 8 ? acc[q + 2][r] : acc[q][r];
+            const float got = __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(
+                0, (int)__float_as_uint(give), 0x128 /* row_ror:8 */, 0xF, 0xF, false));
+            row[EPL * (4 * g + r) + 8 * q] = own + got;
+        }
     return block_finish<F, LPR, WAVES>(red, partial, meet, gtile, y, tile, col0, tile_cols, join.slice(s),
                                        join.slices(splits), n, a, report, cnt, join.grid_threshold(t), join);
 }
