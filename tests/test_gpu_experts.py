@@ -119,6 +119,48 @@ def test_route_of_masked_infinite_and_nan_logits(T, sigmoid, biased, groups):   
             check_route(T, logits[rows], bias, sigmoid, groups, top_groups, group_top, 6, renormalise, 1.0)
 
 
+@pytest.mark.parametrize("tokens", [40, 8195])
+@pytest.mark.parametrize("experts,groups,top_groups,group_top,top_k", [(256, 8, 4, 2, 8), (64, 1, 1, 1, 6), (128, 4, 2, 1, 15),
+                                                                      (1000, 1, 1, 1, 8), (60, 5, 2, 2, 4)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_route_of_scores_next_to_each_other(T, tokens, experts, groups, top_groups, group_top, top_k, sigmoid):   # noqa: F811
+    """Sums of score and bias that differ by less than an fp32 score can tell, in experts and in groups, and equal ones;
+    biases much larger than the scores."""
+    rng = np.random.default_rng(experts + tokens)
+    z = rng.standard_normal(experts).astype(np.float32)
+    score = 1 / (1 + np.exp(-z.astype(np.float64)))
+    bias = (0.75 - score).astype(np.float32)                   # with sigmoid scores all sums are 0.75 to within 2^-25
+    logits = np.tile(z, (tokens, 1))
+    logits[1::4] += (1e-7 * rng.integers(-3, 4, (len(logits[1::4]), experts))).astype(np.float32)
+    logits[2::4] += rng.standard_normal((len(logits[2::4]), experts)).astype(np.float32)
+    logits[3::4] = 0.25
+    for b in (bias, 1000 * bias, np.where(np.arange(experts) % 7 == 0, np.float32(1e30), bias).astype(np.float32), None):
+        check_route(T, logits, b, sigmoid, groups, top_groups, group_top, top_k, True, 1.0)
+
+
+@pytest.mark.parametrize("experts,groups,top_groups,group_top,top_k", [(256, 8, 4, 2, 8), (128, 1, 1, 1, 8), (64, 8, 3, 1, 15),
+                                                                      (60, 1, 1, 1, 4), (256, 1, 1, 1, 17), (512, 8, 2, 2, 6)])
+@pytest.mark.parametrize("sigmoid,biased", [(False, False), (False, True), (True, False), (True, True)])
+def test_route_of_many_tokens(T, experts, groups, top_groups, group_top, top_k, sigmoid, biased):   # noqa: F811
+    rng = np.random.default_rng(experts)
+    logits = (1.5 * rng.standard_normal((8194, experts))).astype(np.float32)
+    logits[100, ::3] = -np.inf
+    logits[8193] = np.nan
+    bias = (0.05 * rng.standard_normal(experts)).astype(np.float32) if biased else None
+    check_route(T, logits, bias, sigmoid, groups, top_groups, group_top, top_k, sigmoid, 2.5)
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_route_with_a_bias_that_is_no_number(T, value, groups):   # noqa: F811
+    rng = np.random.default_rng(9)
+    logits = rng.standard_normal((6, 64)).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(64)).astype(np.float32)
+    bias[[3, 40]] = value
+    idx, _ = run_route(T, logits, bias, True, groups, max(1, groups // 2), 1, 6, True, 1.0)
+    assert np.array_equal(idx, route_reference(logits, bias, True, groups, max(1, groups // 2), 1, 6, True, 1.0)[0])
+
+
 def test_route_in_a_graph_and_on_another_stream(T):   # noqa: F811
     rng = np.random.default_rng(8)
     first, second = rng.standard_normal((2, 8, 128)).astype(np.float32)
