@@ -34,7 +34,7 @@ constexpr int kTraceBlocks = 8192, kTraceMarks = 8;
 static __device__ unsigned long long teal_trace[kTraceBlocks * kTraceMarks];
 __device__ __forceinline__ void trace_mark_thread(int slot, int thread)
 {
-    const int block = blockIdx.x + blockIdx.y * gridDim.x;
+    const int block = blockIdx.x + (blockIdx.y + blockIdx.z * gridDim.y) * gridDim.x;
     if ((int)threadIdx.x == thread && block < kTraceBlocks)
         teal_trace[block * kTraceMarks + slot] = wall_clock64();
 }

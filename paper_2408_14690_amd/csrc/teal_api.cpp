@@ -201,7 +201,9 @@ GemvShape mx4_shape(int m, const int *n, int count)
 
 // The products of `copies` (token, expert) pairs, each with `count` matrices; `joined` of them meet in one sum of y.
 // As shape_for_multi, with several rounds of blocks allowed (a batch's pairs alone may be more than the units)
-// and no more slices to a sum than meet in column words.
+// and no more slices to a sum than meet in column words.  Tiles have from min_cols to all of max_lanes' columns in
+// steps of whole lines: with 192 bytes of a row, mx4 experts of 768 columns, neighbours fetch a line twice (us, 56
+// pairs of 2048 x 2 x 768: 384 columns 16.2, 512, the second of a matrix half empty, 15.1).
 GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, int elems_per_lane, int min_cols,
                         int step, int max_lanes)
 {
@@ -1390,7 +1392,7 @@ static teal_status experts_call(int bits, teal::ExpertHostArgs h, void *workspac
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bits == 16)
         return from_hip(teal::launch_experts_bf16(h, experts_shape(pairs, h.m, h.n, h.count, joined, 8, 128, 64, 64), st));
-    return from_hip(teal::launch_experts_mx4(h, experts_shape(pairs, h.m, h.n, h.count, joined, 32, 256, 128, 16), st));
+    return from_hip(teal::launch_experts_mx4(h, experts_shape(pairs, h.m, h.n, h.count, joined, 32, 512, 512, 16), st));
 }
 
 static teal::ExpertHostArgs experts_args(int count, const void *const *W, const void *const *scale,
