@@ -249,25 +249,23 @@ def load_library():
 def _ptr(a, need=None, what="argument"):
     """Device address of a tensor (or a raw address).  With `need`, a tensor smaller than
     that many bytes is refused here: the C ABI sees plain pointers and cannot know."""
-    if a is None:
-        return None
-    if isinstance(a, int):
+    if a is None or isinstance(a, int):
         return a
-    if hasattr(a, "data_ptr"):
+    try:
         if not a.is_contiguous():
             raise ValueError("tensor arguments must be contiguous")
-        if need is not None and a.numel() * a.element_size() < int(need):
-            raise ValueError(f"{what}: tensor of {a.numel() * a.element_size()} bytes, "
-                             f"the call reads or writes {int(need)}")
+        if need is not None and a.nbytes < need:
+            raise ValueError(f"{what}: tensor of {a.nbytes} bytes, the call reads or writes {int(need)}")
         return a.data_ptr()
-    raise TypeError(f"cannot pass {type(a).__name__} as a device pointer")
+    except AttributeError:
+        raise TypeError(f"cannot pass {type(a).__name__} as a device pointer") from None
 
 
 def _nbytes(a, given):
     if given is not None:
         return int(given)
     if hasattr(a, "numel"):
-        return a.numel() * a.element_size()
+        return a.nbytes
     raise TypeError("workspace_bytes is required when workspace is a raw address")
 
 
@@ -291,7 +289,7 @@ def _call(name, *cargs):
     """Every call that enqueues GPU work goes through here: normally straight into the
     library; while prepare() records on the calling thread, the marshalled arguments are kept
     instead.  Calls from other host threads are not affected by a recording."""
-    fn = getattr(load_library(), name)
+    fn = getattr(_lib or load_library(), name)
     recording = getattr(_tls, "recording", None)
     if recording is not None:
         recording.append((fn, cargs))
@@ -902,16 +900,28 @@ def teal_sparse_gemv_mx4(Wq, scale, x_f16, t, y, m, n, workspace, workspace_byte
         _ptr(y, 4 * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
+# host arrays of up to four entries: their types are looked up by length, which is quicker than asking ctypes for one
+_POINTERS = tuple(ctypes.c_void_p * k for k in range(5))
+_INTS = tuple(ctypes.c_int * k for k in range(5))
+
+
+def _pointers(values, count):
+    return (_POINTERS[count] if count < 5 else ctypes.c_void_p * count)(*values)
+
+
+def _ints(values, count):
+    return (_INTS[count] if count < 5 else ctypes.c_int * count)(*map(int, values))
+
+
 def _mx4_arrays(Wq_list, scale_list, y_list, n_list, m, experts=1, rows=1):
     """Host arrays of a grouped call; `experts` matrices and `rows` output rows per entry."""
     count = len(Wq_list)
     if not (len(scale_list) == len(y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
-    W = (ctypes.c_void_p * count)(*[_ptr(w, experts * (m * n // 2), "Wq") for w, n in zip(Wq_list, n_list)])
-    S = (ctypes.c_void_p * count)(*[_ptr(sc, experts * _mx4_scale_need(m, n), "scale")
-                                    for sc, n in zip(scale_list, n_list)])
-    Y = (ctypes.c_void_p * count)(*[_ptr(y, 4 * rows * n, "y") for y, n in zip(y_list, n_list)])
-    N = (ctypes.c_int * count)(*[int(n) for n in n_list])
+    W = _pointers([_ptr(w, experts * (m * n // 2), "Wq") for w, n in zip(Wq_list, n_list)], count)
+    S = _pointers([_ptr(sc, experts * _mx4_scale_need(m, n), "scale") for sc, n in zip(scale_list, n_list)], count)
+    Y = _pointers([_ptr(y, 4 * rows * n, "y") for y, n in zip(y_list, n_list)], count)
+    N = _ints(n_list, count)
     return count, W, S, Y, N
 
 
@@ -966,7 +976,7 @@ def teal_workspace_bytes_experts(m: int, n: int, pairs: int) -> int:
 def _expert_thresholds(t_list, count, experts):
     if len(t_list) != count:
         raise ValueError("per-matrix lists must have the same length")
-    return (ctypes.c_void_p * count)(*[_ptr(t, 4 * experts, "t") for t in t_list])
+    return _pointers([_ptr(t, 4 * experts, "t") for t in t_list], count)
 
 
 def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, tokens, top_k, X_f16, m, workspace,
@@ -975,9 +985,9 @@ def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, toke
     count = len(Wt_list)
     if not (len(y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
-    W = (ctypes.c_void_p * count)(*[_ptr(w, 2 * experts * m * n, "Wt") for w, n in zip(Wt_list, n_list)])
-    Y = (ctypes.c_void_p * count)(*[_ptr(y, 4 * tokens * top_k * n, "y") for y, n in zip(y_list, n_list)])
-    N = (ctypes.c_int * count)(*[int(n) for n in n_list])
+    W = _pointers([_ptr(w, 2 * experts * m * n, "Wt") for w, n in zip(Wt_list, n_list)], count)
+    Y = _pointers([_ptr(y, 4 * tokens * top_k * n, "y") for y, n in zip(y_list, n_list)], count)
+    N = _ints(n_list, count)
     return _call(
         "teal_sparse_experts_bf16",
         count, W, _expert_thresholds(t_list, count, experts), Y, N, int(experts),
