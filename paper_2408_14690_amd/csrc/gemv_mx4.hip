@@ -394,9 +394,14 @@ hipError_t launch_experts_mx4(const ExpertHostArgs &h, const GemvShape &sh, hipS
 constexpr int kMx4PackRows = 128, kMx4PackWaves = 4;
 
 // Two bf16 values of neighbouring channels; a row of W begins on an even address only.
-struct __attribute__((packed, aligned(2))) Mx4Pair {
-    unsigned v;
-};
+typedef unsigned Mx4Pair __attribute__((aligned(2)));
+
+// W past the caches, where that pays.  Written, if rows begin on cache lines, so that a wavefront writes whole ones
+// (unpack of 8192 x 28672 123 -> 89 us, 4096 x 14336 23.7 -> 22.6; where they do not, 5001 x 3424, it would be 10.6 ->
+// 17.8).  Read, if moreover W is larger than the last cache and so cannot come from it (pack of 8192 x 28672
+// 126 -> 111 us; 4096 x 14336 just written 22 -> 29).
+constexpr size_t kLastCache = (size_t)256 << 20;
+inline bool mx4_whole_lines(const void *W, int m) { return m % 64 == 0 && (reinterpret_cast<uintptr_t>(W) & 127) == 0; }
 
 struct Mx4PackTile {
     u32x4 codes[kMx4PackRows][kMx4PackWaves + 1];     // one of padding: lanes two channels apart do not meet in a bank
@@ -412,6 +417,7 @@ __device__ __forceinline__ size_t mx4_scale_place(int i, int b, int n)
     return ((size_t)(i / 8) * mx4_scale_tiles(n) + b / 16) * kMx4TileBytes + i % 8 * 16 + b % 16;
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint16_t *__restrict__ W,
                                                                       uint8_t *__restrict__ Wq,
                                                                       uint8_t *__restrict__ scale, int m, int n,
@@ -426,12 +432,15 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint
         const uint16_t *first = W + (size_t)(b0 + w) * 32 * m;
         if (i0 + kMx4PackRows <= m) {
 #pragma unroll
-            for (int r = 0; r < 32; ++r) v[r] = reinterpret_cast<const Mx4Pair *>(first + (size_t)r * m + i)->v;
+            for (int r = 0; r < 32; ++r) {
+                const Mx4Pair *p = reinterpret_cast<const Mx4Pair *>(first + (size_t)r * m + i);
+                v[r] = PAST ? __builtin_nontemporal_load(p) : *p;
+            }
         } else {
 #pragma unroll
             for (int r = 0; r < 32; ++r) {
                 const uint16_t *p = first + (size_t)r * m + i;
-                v[r] = i + 1 < m ? reinterpret_cast<const Mx4Pair *>(p)->v : i < m ? *p : 0u;
+                v[r] = i + 1 < m ? *reinterpret_cast<const Mx4Pair *>(p) : i < m ? *p : 0u;
             }
         }
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -485,6 +494,7 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint
                 b == b0 ? *reinterpret_cast<const unsigned *>(tile.scale[c]) : 0u;
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kMx4PackWaves * 64) void unpack_mx4_kernel(const uint8_t *__restrict__ Wq,
                                                                         const uint8_t *__restrict__ scale,
                                                                         uint16_t *__restrict__ W, int m, int n,
@@ -531,7 +541,9 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void unpack_mx4_kernel(const ui
 #pragma unroll
     for (int r = 0; r < 32; ++r) {
         const unsigned v = __builtin_amdgcn_perm(two[1][r / 2], two[0][r / 2], r % 2 ? 0x07060302u : 0x05040100u);
-        if (both) reinterpret_cast<Mx4Pair *>(first + (size_t)r * m)->v = v;
+        Mx4Pair *p = reinterpret_cast<Mx4Pair *>(first + (size_t)r * m);
+        if (PAST) __builtin_nontemporal_store(v, p);                  // an even number of channels
+        else if (both) *p = v;
         else first[(size_t)r * m] = (uint16_t)v;
     }
 }
@@ -551,8 +563,9 @@ hipError_t launch_pack_mx4(const void *W, uint8_t *Wq, uint8_t *scale, int m, in
 {
     const Mx4LayoutGrid g(m, n);
     if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;      // more weights than a GPU has bytes
-    hipLaunchKernelGGL(pack_mx4_kernel, dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream,
-                       static_cast<const uint16_t *>(W), Wq, scale, m, n, g.tiles_m);
+    const bool past = mx4_whole_lines(W, m) && (size_t)m * n * sizeof(uint16_t) > kLastCache;
+    hipLaunchKernelGGL(past ? pack_mx4_kernel<true> : pack_mx4_kernel<false>, dim3((unsigned)g.tiles),
+                       dim3(kMx4PackWaves * 64), 0, stream, static_cast<const uint16_t *>(W), Wq, scale, m, n, g.tiles_m);
     return hipGetLastError();
 }
 
@@ -560,7 +573,8 @@ hipError_t launch_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W, i
 {
     const Mx4LayoutGrid g(m, n);
     if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(unpack_mx4_kernel, dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream, Wq, scale,
+    hipLaunchKernelGGL(mx4_whole_lines(W, m) ? unpack_mx4_kernel<true> : unpack_mx4_kernel<false>,
+                       dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream, Wq, scale,
                        static_cast<uint16_t *>(W), m, n, g.tiles_m);
     return hipGetLastError();
 }
