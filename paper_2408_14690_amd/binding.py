@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 TEAL_OK = 0
@@ -208,7 +209,6 @@ def load_library():
     lib.teal_sparse_mlp_w4.restype = i
     lib.teal_sparse_mlp_w4.argtypes = [vp, vp, vp, vp, vp, vp, i, vp, f, f, f, vp, vp, vp, i, i, i,
                                        vp, sz, vp, shp]
-    vpp, fp, ipp = c.POINTER(vp), c.POINTER(f), c.POINTER(i)
     lib.teal_mx4_scale_bytes.restype = sz
     lib.teal_mx4_scale_bytes.argtypes = [i, i]
     lib.teal_pack_mx4.restype = i
@@ -218,19 +218,19 @@ def load_library():
     lib.teal_sparse_gemv_mx4.restype = i
     lib.teal_sparse_gemv_mx4.argtypes = [vp, vp, vp, f, vp, i, i, vp, sz, vp]
     lib.teal_sparse_gemv_mx4_multi.restype = i
-    lib.teal_sparse_gemv_mx4_multi.argtypes = [i, vpp, vpp, fp, vpp, ipp, vp, i, vp, sz, vp]
+    lib.teal_sparse_gemv_mx4_multi.argtypes = [i, vp, vp, vp, vp, vp, vp, i, vp, sz, vp]
     lib.teal_sparse_gemv_mx4_swiglu.restype = i
     lib.teal_sparse_gemv_mx4_swiglu.argtypes = [vp, vp, vp, vp, f, vp, i, i, vp, sz, vp]
     lib.teal_sparse_gemv_mx4_rmsnorm_multi.restype = i
-    lib.teal_sparse_gemv_mx4_rmsnorm_multi.argtypes = [i, vpp, vpp, fp, vpp, ipp, vp, vp, f, i, vp, sz, vp]
+    lib.teal_sparse_gemv_mx4_rmsnorm_multi.argtypes = [i, vp, vp, vp, vp, vp, vp, vp, f, i, vp, sz, vp]
     lib.teal_route_experts.restype = i
     lib.teal_route_experts.argtypes = [vp, vp, i, i, i, i, i, i, i, i, f, vp, vp, vp]
     lib.teal_workspace_bytes_experts.restype = sz
     lib.teal_workspace_bytes_experts.argtypes = [i, i, i]
     lib.teal_sparse_experts_bf16.restype = i
-    lib.teal_sparse_experts_bf16.argtypes = [i, vpp, vpp, vpp, ipp, i, vp, i, i, vp, i, vp, sz, vp]
+    lib.teal_sparse_experts_bf16.argtypes = [i, vp, vp, vp, vp, i, vp, i, i, vp, i, vp, sz, vp]
     lib.teal_sparse_experts_mx4.restype = i
-    lib.teal_sparse_experts_mx4.argtypes = [i, vpp, vpp, vpp, vpp, ipp, i, vp, i, i, vp, i, vp, sz, vp]
+    lib.teal_sparse_experts_mx4.argtypes = [i, vp, vp, vp, vp, vp, i, vp, i, i, vp, i, vp, sz, vp]
     lib.teal_sparse_experts_bf16_swiglu.restype = i
     lib.teal_sparse_experts_bf16_swiglu.argtypes = [vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp, sz, vp]
     lib.teal_sparse_experts_mx4_swiglu.restype = i
@@ -269,14 +269,25 @@ def _nbytes(a, given):
     raise TypeError("workspace_bytes is required when workspace is a raw address")
 
 
+def _find_current_stream():
+    """The function that gives the address of torch's current stream.  The address alone: a Stream object for it takes
+    2.9 us, as long as a small kernel."""
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+    if raw is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(device())
+
+
+_current_stream = None
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        # the address alone: a Stream object for it takes 2.9 us, more than the launch of a kernel's arguments
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None:
-            return raw(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+        global _current_stream
+        if _current_stream is None:
+            _current_stream = _find_current_stream()
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -900,17 +911,27 @@ def teal_sparse_gemv_mx4(Wq, scale, x_f16, t, y, m, n, workspace, workspace_byte
         _ptr(y, 4 * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
-# host arrays of up to four entries: their types are looked up by length, which is quicker than asking ctypes for one
-_POINTERS = tuple(ctypes.c_void_p * k for k in range(5))
-_INTS = tuple(ctypes.c_int * k for k in range(5))
+# Host arrays as bytes, which ctypes passes by their address: less host time than ctypes arrays.
+_pack_pointers, _pack_ints, _pack_floats = (
+    tuple(struct.Struct(f"{count}{kind}").pack for count in range(5)) for kind in "Pif")
 
 
-def _pointers(values, count):
-    return (_POINTERS[count] if count < 5 else ctypes.c_void_p * count)(*values)
+def _pointers(values):
+    if len(values) < 5:
+        return _pack_pointers[len(values)](*values)
+    return struct.pack(f"{len(values)}P", *values)
 
 
-def _ints(values, count):
-    return (_INTS[count] if count < 5 else ctypes.c_int * count)(*map(int, values))
+def _ints(values):
+    if len(values) < 5:
+        return _pack_ints[len(values)](*values)
+    return struct.pack(f"{len(values)}i", *values)
+
+
+def _floats(values):
+    if len(values) < 5:
+        return _pack_floats[len(values)](*values)
+    return struct.pack(f"{len(values)}f", *values)
 
 
 def _mx4_arrays(Wq_list, scale_list, y_list, n_list, m, experts=1, rows=1):
@@ -918,10 +939,10 @@ def _mx4_arrays(Wq_list, scale_list, y_list, n_list, m, experts=1, rows=1):
     count = len(Wq_list)
     if not (len(scale_list) == len(y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
-    W = _pointers([_ptr(w, experts * (m * n // 2), "Wq") for w, n in zip(Wq_list, n_list)], count)
-    S = _pointers([_ptr(sc, experts * _mx4_scale_need(m, n), "scale") for sc, n in zip(scale_list, n_list)], count)
-    Y = _pointers([_ptr(y, 4 * rows * n, "y") for y, n in zip(y_list, n_list)], count)
-    N = _ints(n_list, count)
+    W = _pointers([_ptr(w, experts * (m * n // 2), "Wq") or 0 for w, n in zip(Wq_list, n_list)])
+    S = _pointers([_ptr(sc, experts * _mx4_scale_need(m, n), "scale") or 0 for sc, n in zip(scale_list, n_list)])
+    Y = _pointers([_ptr(y, 4 * rows * n, "y") or 0 for y, n in zip(y_list, n_list)])
+    N = _ints(n_list)
     return count, W, S, Y, N
 
 
@@ -931,7 +952,7 @@ def teal_sparse_gemv_mx4_multi(Wq_list, scale_list, t_list, y_list, n_list, x_f1
     count, W, S, Y, N = _mx4_arrays(Wq_list, scale_list, y_list, n_list, m)
     if len(t_list) != count:
         raise ValueError("per-matrix lists must have the same length")
-    Tt = (ctypes.c_float * count)(*[float(t) for t in t_list])
+    Tt = _floats(t_list)
     return _call(
         "teal_sparse_gemv_mx4_multi",
         count, W, S, Tt, Y, N, _ptr(x_f16, 2 * m, "x"), int(m), _ptr(workspace),
@@ -952,7 +973,7 @@ def teal_sparse_gemv_mx4_rmsnorm_multi(Wq_list, scale_list, t_list, y_list, n_li
     count, W, S, Y, N = _mx4_arrays(Wq_list, scale_list, y_list, n_list, m)
     if len(t_list) != count:
         raise ValueError("per-matrix lists must have the same length")
-    Tt = (ctypes.c_float * count)(*[float(t) for t in t_list])
+    Tt = _floats(t_list)
     return _call(
         "teal_sparse_gemv_mx4_rmsnorm_multi",
         count, W, S, Tt, Y, N, _ptr(h, 4 * m, "h"), _ptr(gamma, 4 * m, "gamma"), float(eps), int(m),
@@ -965,7 +986,7 @@ def teal_route_experts(logits, bias, score, tokens, experts, groups, top_groups,
         "teal_route_experts",
         _ptr(logits, 4 * tokens * experts, "logits"), _ptr(bias, 4 * experts, "bias"), int(score), int(tokens),
         int(experts), int(groups), int(top_groups), int(group_top), int(top_k), int(bool(renormalise)),
-        float(scaling), _ptr(idx, 4 * tokens * top_k, "idx"), _ptr(weight, 4 * tokens * top_k, "weight"),
+        float(scaling), _expert_numbers(idx, tokens * top_k), _ptr(weight, 4 * tokens * top_k, "weight"),
         _stream(stream))
 
 
@@ -973,10 +994,16 @@ def teal_workspace_bytes_experts(m: int, n: int, pairs: int) -> int:
     return int(load_library().teal_workspace_bytes_experts(int(m), int(n), int(pairs)))
 
 
+def _expert_numbers(idx, pairs):
+    if getattr(idx, "element_size", None) is not None and idx.element_size() != 4:
+        raise ValueError("idx: the experts' numbers are 32-bit integers")       # (torch.topk gives 64-bit ones)
+    return _ptr(idx, 4 * pairs, "idx")
+
+
 def _expert_thresholds(t_list, count, experts):
     if len(t_list) != count:
         raise ValueError("per-matrix lists must have the same length")
-    return _pointers([_ptr(t, 4 * experts, "t") for t in t_list], count)
+    return _pointers([_ptr(t, 4 * experts, "t") or 0 for t in t_list])
 
 
 def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, tokens, top_k, X_f16, m, workspace,
@@ -985,13 +1012,13 @@ def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, toke
     count = len(Wt_list)
     if not (len(y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
-    W = _pointers([_ptr(w, 2 * experts * m * n, "Wt") for w, n in zip(Wt_list, n_list)], count)
-    Y = _pointers([_ptr(y, 4 * tokens * top_k * n, "y") for y, n in zip(y_list, n_list)], count)
-    N = _ints(n_list, count)
+    W = _pointers([_ptr(w, 2 * experts * m * n, "Wt") or 0 for w, n in zip(Wt_list, n_list)])
+    Y = _pointers([_ptr(y, 4 * tokens * top_k * n, "y") or 0 for y, n in zip(y_list, n_list)])
+    N = _ints(n_list)
     return _call(
         "teal_sparse_experts_bf16",
         count, W, _expert_thresholds(t_list, count, experts), Y, N, int(experts),
-        _ptr(idx, 4 * tokens * top_k, "idx"), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
+        _expert_numbers(idx, tokens * top_k), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
         _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -1001,7 +1028,7 @@ def teal_sparse_experts_mx4(Wq_list, scale_list, t_list, y_list, n_list, experts
     return _call(
         "teal_sparse_experts_mx4",
         count, W, S, _expert_thresholds(t_list, count, experts), Y, N, int(experts),
-        _ptr(idx, 4 * tokens * top_k, "idx"), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
+        _expert_numbers(idx, tokens * top_k), int(tokens), int(top_k), _ptr(X_f16, 2 * tokens * m, "X"), int(m),
         _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -1011,7 +1038,7 @@ def teal_sparse_experts_bf16_swiglu(Wt_bf16, t, y, experts, idx, weight, tokens,
     return _call(
         "teal_sparse_experts_bf16_swiglu",
         _ptr(Wt_bf16, 2 * experts * m * n, "Wt"), _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"),
-        int(experts), _ptr(idx, 4 * pairs, "idx"), _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k),
+        int(experts), _expert_numbers(idx, pairs), _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k),
         _ptr(gate, 4 * pairs * m, "gate"), _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace),
         _nbytes(workspace, workspace_bytes), _stream(stream))
 

@@ -177,5 +177,10 @@ def test_tensors_that_are_too_small_or_not_contiguous_are_refused():
     with pytest.raises(ValueError):
         T.teal_sparse_experts_mx4([q], [s], [torch.zeros(2)], [torch.zeros(2, 64)], [64], 2, idx[:1, :2].contiguous(), 1, 2,
                                   x, 64, WS, BIG, stream=0)        # one expert's weights for two
+    with pytest.raises(ValueError):                                # 64-bit numbers of experts, as torch.topk gives them
+        T.teal_sparse_experts_mx4([q], [s], [torch.zeros(1)], [torch.zeros(64)], [64], 1, torch.zeros(1, 1, dtype=torch.int64),
+                                  1, 1, x, 64, WS, BIG, stream=0)
+    with pytest.raises(ValueError):
+        T.teal_route_experts(logits, None, 0, 4, 8, 1, 1, 1, 2, True, 1.0, idx.long(), weight, stream=0)
     with pytest.raises(ValueError):
         T.teal_sparse_gemv_mx4_multi([q, q], [s], [0.5, 0.5], [y, y], [64, 64], x, 64, WS, BIG, stream=0)
