@@ -1,7 +1,7 @@
 // The products of a mixture of experts: every token of a small batch goes through the top_k experts that its
 // router chose, and their numbers are on the device.  A block reads the number of its expert and takes that
-// expert's matrix and threshold; it is otherwise a block of the dense products (Body::run, gemv_mlp.h), so a
-// token's product with one expert is what the plain call gives on that expert's matrix.
+// expert's matrix and threshold; it is otherwise a block of the products of one matrix (Body::run, gemv_mlp.h), so a
+// token's product with one expert is, up to the order of the sums, what the plain call gives on its matrix.
 #pragma once
 
 #include "gemv_common.h"

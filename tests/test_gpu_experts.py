@@ -150,6 +150,23 @@ def test_route_of_many_tokens(T, experts, groups, top_groups, group_top, top_k, 
     check_route(T, logits, bias, sigmoid, groups, top_groups, group_top, top_k, sigmoid, 2.5)
 
 
+@pytest.mark.parametrize("experts,groups", [(64, 1), (400, 1), (256, 8), (15, 1), (48, 3)])
+def test_route_of_logits_that_begin_anywhere(T, experts, groups):   # noqa: F811
+    rng = np.random.default_rng(experts)
+    logits = rng.standard_normal((21, experts)).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(experts)).astype(np.float32)
+    room = torch.empty(21 * experts + experts + 8, device="cuda")
+    idx, weight = torch.empty(21, 4, dtype=torch.int32, device="cuda"), torch.empty(21, 4, device="cuda")
+    for shift in range(4):
+        z, b = room[shift:shift + 21 * experts], room[21 * experts + 4 + shift % 2:][:experts]
+        z.copy_(dev(logits.ravel()))
+        b.copy_(dev(bias))
+        for used in (None, b):
+            T.check(T.teal_route_experts(z, used, 1, 21, experts, groups, groups, 1, 4, True, 1.0, idx, weight))
+            how = (True, groups, groups, 1, 4, True, 1.0)
+            assert np.array_equal(idx.cpu().numpy(), route_reference(logits, None if used is None else bias, *how)[0])
+
+
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("groups", [1, 4])
 def test_route_with_a_bias_that_is_no_number(T, value, groups):   # noqa: F811
@@ -218,7 +235,8 @@ def product(x, t, values):
     """(product, bound of its error) of one token and expert."""
     kept = np.abs(x.astype(np.float64)) > t
     xk, wk = x[kept].astype(np.float64), values[kept]
-    return xk @ wk, (kept.sum() / 8 + 65) * 2.0 ** -24 * (np.abs(xk) @ np.abs(wk))
+    with np.errstate(invalid="ignore"):                      # (infinite inputs)
+        return xk @ wk, (kept.sum() / 8 + 65) * 2.0 ** -24 * (np.abs(xk) @ np.abs(wk))
 
 
 def choose(rng, tokens, experts, top_k):
@@ -231,7 +249,8 @@ def choose(rng, tokens, experts, top_k):
 
 SIZES = [(1, 4, 1, 64, [32], 0.5), (1, 8, 2, 1000, [96, 352], 0.5), (3, 5, 2, 129, [64, 64], 0.0), (8, 16, 4, 513, [544, 96], 0.5),
          (2, 3, 2, 4500, [256], 0.8), (8, 4, 8, 640, [768, 768], 0.5), (4, 2, 3, 2048, [1024, 1024, 64, 32], 0.95),
-         (8, 3, 32, 200, [1056], 0.5), (1, 2, 2, 2048, [4096, 4096], 0.5), (5, 6, 1, 33, [64], 1.0)]
+         (8, 3, 32, 200, [1056], 0.5), (1, 2, 2, 2048, [4096, 4096], 0.5), (5, 6, 1, 33, [64], 1.0),
+         (8, 3, 8, 4200, [1536, 1536], 0.9), (1, 2, 1, 70001, [32], 0.5), (2, 1, 1, 8200, [96, 64], 0.25)]
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mx4"])
@@ -267,7 +286,8 @@ def test_experts_against_binary64(T, fmt, tokens, experts, top_k, m, widths, p):
 
 DOWN = [(1, 4, 1, 64, 32, 0.5), (1, 8, 2, 1000, 96, 0.5), (3, 5, 2, 129, 544, 0.0), (8, 16, 4, 513, 1056, 0.5),
         (2, 3, 2, 4500, 256, 0.8), (8, 4, 8, 768, 2048, 0.5), (1, 2, 32, 640, 64, 0.5), (1, 3, 8, 20000, 64, 0.5),
-        (4, 3, 2, 2048, 512, 0.95), (1, 2, 2, 3584, 1024, 0.5), (5, 6, 1, 33, 64, 1.0)]
+        (4, 3, 2, 2048, 512, 0.95), (1, 2, 2, 3584, 1024, 0.5), (5, 6, 1, 33, 64, 1.0),
+        (8, 3, 8, 4200, 2048, 0.9), (1, 2, 1, 70001, 32, 0.5), (8, 2, 32, 130, 1024, 0.5)]
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mx4"])
@@ -306,6 +326,66 @@ def test_experts_down_against_binary64(T, fmt, tokens, experts, top_k, m, n, p):
     for _ in range(2):
         ex.down(T, *args)
         assert torch.equal(first, y)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("tokens,top_k,m,n", [(8, 8, 4200, 1536), (1, 32, 640, 64), (1, 8, 20000, 64), (8, 32, 130, 1024), (2, 2, 2048, 512),
+                                              (3, 1, 9000, 2048)])
+def test_a_workspace_is_as_large_as_it_is_said_to_be(T, fmt, tokens, top_k, m, n):   # noqa: F811
+    """Sums of unusual size take the way through the partial rows in every launch shape: nothing behind the workspace is
+    written, and the next call, of other sizes, finds it as it should be."""
+    ex, down = Experts(fmt, 2, m, [n], 3), Experts(fmt, 2, m, [n], 4)
+    rng = np.random.default_rng(6)
+    need = T.teal_workspace_bytes_experts(m, n, tokens * top_k)
+    room = torch.full((need + 4096,), 0xEE, dtype=torch.uint8, device="cuda")
+    ws = room[:need]
+    ws.zero_()
+    idx = dev(rng.integers(0, 2, (tokens, top_k)).astype(np.int32))
+    t = torch.zeros(2, device="cuda")
+    for size in (2.0 ** -14, 1.0, 2.0 ** 13):
+        x = (rng.standard_normal((tokens, m)) * size).astype(np.float16)
+        y = torch.empty(tokens, top_k, n, device="cuda")
+        ex(T, [t], [y], idx, dev(x), ws)
+        gate, up = rng.standard_normal((2, tokens, top_k, m)).astype(np.float32)
+        up *= np.float32(size)
+        z = torch.empty(tokens, n, device="cuda")
+        weight = torch.full((tokens, top_k), 0.75, device="cuda")
+        down.down(T, t, z, idx, weight, dev(gate), dev(up), ws)
+        chosen = idx.cpu().numpy()
+        h = torch.empty(tokens, top_k, m, dtype=torch.float16, device="cuda")
+        T.check(T.teal_swiglu_f16(dev(gate), dev(up), h, h.numel()))
+        h = h.cpu().numpy()
+        for b in (0, tokens - 1):
+            want, bound = product(x[b], 0, ex.values[0][chosen[b, 0]])
+            assert np.all(np.abs(y[b, 0].cpu().numpy() - want) <= bound)
+            parts = [product(h[b, j], 0, down.values[0][chosen[b, j]]) for j in range(top_k)]
+            want, off = 0.75 * sum(w for w, _ in parts), sum(o for _, o in parts)
+            # what more than 32 slices are added in fp32 with is, slice by slice, within a last place of sums whose
+            # magnitudes the bounds of the products have too
+            got = z[b].cpu().numpy()
+            with np.errstate(invalid="ignore"):              # (some h are infinite: then so is what has to come out)
+                assert np.all((got == want) | np.isnan(got) & np.isnan(want) | (np.abs(got - want) <= off * (1 + 16 * top_k / 65)) & np.isfinite(want))
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xEE).all())
+    assert not bool(ws[:T.teal_survivors_offset()].any())           # ready for the next call
+
+
+def test_experts_on_two_streams(T):   # noqa: F811
+    ex = Experts("mx4", 6, 1024, [512, 512], 2)
+    rng = np.random.default_rng(2)
+    x, idx = dev(rng.standard_normal((4, 1024)).astype(np.float16)), dev(rng.integers(0, 6, (4, 2)).astype(np.int32))
+    t = [torch.full((6,), 0.7, device="cuda")] * 2
+    spaces = [expert_workspace(T, 1024, 1024, 8) for _ in range(2)]
+    ys = [[torch.empty(4, 2, 512, device="cuda") for _ in range(2)] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, ws, y in zip(streams, spaces, ys):
+            ex(T, t, y, idx, x, ws, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*ys))
+    want, bound = product(x[3].cpu().numpy(), float(t[0][0]), ex.values[1][int(idx[3, 1])])
+    assert np.all(np.abs(ys[0][1][3, 1].cpu().numpy() - want) <= bound)
 
 
 def test_thresholds_that_no_call_would_accept_count_as_zero(T):   # noqa: F811

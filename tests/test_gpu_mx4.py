@@ -193,7 +193,7 @@ def test_infinite_inputs_and_nan_blocks(T):
     q, s, ws, y = dev(codes), dev(scales), workspace(T, m, n), torch.empty(n, device="cuda")
     x[500] = np.inf
     T.check(T.teal_sparse_gemv_mx4(q, s, dev(x), t, y, m, n, ws))
-    want = np.where(values[500] == 0, np.nan, np.sign(values[500]) * np.inf)
+    want = np.where(values[500] == 0, np.nan, np.copysign(np.inf, values[500]))
     assert np.array_equal(y.cpu().numpy(), want, equal_nan=True)
     # a NaN block of a channel that is kept is NaN in its 32 columns, of one that is dropped in none
     x[500], x[17] = 3.0, 0.0
