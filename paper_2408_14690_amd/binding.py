@@ -273,8 +273,9 @@ def _find_current_stream():
     """The function that gives the address of torch's current stream.  The address alone: a Stream object for it takes
     2.9 us, as long as a small kernel."""
     import torch
-    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
-    if raw is None:
+    torch.cuda.current_device()                   # initialises, or says why it cannot
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
         return lambda: torch.cuda.current_stream().cuda_stream
     return lambda: raw(device())
 
