@@ -199,18 +199,23 @@ GemvShape mx4_shape(int m, const int *n, int count)
     return sh;
 }
 
-// The products of `copies` (token, expert) pairs, each with `count` matrices; `joined` of them meet in one sum of y.
-// As shape_for_multi, with several rounds of blocks allowed (a batch's pairs alone may be more than the units)
-// and no more slices to a sum than meet in column words.  Tiles have from min_cols to all of max_lanes' columns in
-// steps of whole lines: with 192 bytes of a row, mx4 experts of 768 columns, neighbours fetch a line twice (us, 56
-// pairs of 2048 x 2 x 768: 384 columns 16.2, 512, the second of a matrix half empty, 15.1).
+// The products of `copies` (token, expert) pairs, each with `count` matrices; the slices of `joined` of them meet in one
+// sum of y.  The cheapest by an estimate in us at 50 %: the whole at the rate of memory (`rate` weights a microsecond
+// and unit, 1/16 more for bf16 in pieces of 256 bytes of a row), or the fullest unit at the 1.18 times as much that one
+// takes by itself, whichever is longer, a little of the other, and 0.05 per slice that meets in a sum.  (us, columns x
+// slices: bf16, 8 experts of 1024 -> 2048 joined 256 x 4 8.1, 128 x 2 6.9; 2 of 14336 -> 4096 512 x 8 26.3, 256 x 8
+// 22.0, 128 x 4 23.1; 2 pairs of 4096 -> 2 x 14336 512 x 1 55.8, x 2 40.6, x 4 42.8; mx4, 2 of 14336 -> 4096 joined in
+// 8 slices 13.7, 16 10.8; 8 pairs of 2048 -> 2 x 1024 in 4 7.0, 8 6.2.)  With more than one slice all blocks are
+// resident at once.  Tiles have from min_cols to all of max_lanes' columns in steps of whole lines: with 192 bytes of a
+// row, mx4 experts of 768 columns, neighbours fetch a line twice (56 pairs of 2048 -> 2 x 768 in 384 columns 16.2, in
+// 512, the second of a matrix half empty, 15.1).
 GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, int elems_per_lane, int min_cols,
-                        int step, int max_lanes)
+                        int step, int max_lanes, double rate)
 {
     double best = -1.0;
     GemvShape sh{16, 1, 16 * elems_per_lane, 8, 4};
-    long long n_total = 0;
-    for (int k = 0; k < count; ++k) n_total += n[k];
+    double weights = 0.0;
+    for (int k = 0; k < count; ++k) weights += (double)n[k] * m * copies;
     for (int tc = max_lanes * elems_per_lane; tc >= min_cols; tc -= step) {
         long long tiles = 0;
         for (int k = 0; k < count; ++k) tiles += (n[k] + tc - 1) / tc;
@@ -224,11 +229,12 @@ GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, 
             if (s * joined > 1 && tiles * copies > (long long)(teal::kCounterBytes / sizeof(int))) continue;
             if (s > 1 && blocks > kComputeUnits && m <= teal::kMaxSlice) continue;
             const long long rounds = (blocks + kComputeUnits - 1) / kComputeUnits;
-            double score = (double)n_total * copies * m / ((double)kComputeUnits * rounds * tc * ks);
-            for (int e = 8; e < s; ++e) score *= 0.97;
-            if (s * joined > teal::kWordSplits) score *= 0.9;
-            if (score > best * 1.001) {
-                best = score;
+            double all = weights / kComputeUnits / rate;
+            if (elems_per_lane == 8 && tc <= 128) all *= 17.0 / 16.0;
+            const double one = (double)rounds * ks * tc / (1.18 * rate);
+            const double cost = (all > one ? all + 0.15 * one : one + 0.15 * all) + 0.05 * s * joined;
+            if (best < 0.0 || cost < best) {
+                best = cost;
                 sh.tile_cols = tc;
                 sh.splits = s;
             }
@@ -1391,8 +1397,8 @@ static teal_status experts_call(int bits, teal::ExpertHostArgs h, void *workspac
     const int joined = down ? h.top_k : 1;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bits == 16)
-        return from_hip(teal::launch_experts_bf16(h, experts_shape(pairs, h.m, h.n, h.count, joined, 8, 128, 64, 64), st));
-    return from_hip(teal::launch_experts_mx4(h, experts_shape(pairs, h.m, h.n, h.count, joined, 32, 512, 512, 16), st));
+        return from_hip(teal::launch_experts_bf16(h, experts_shape(pairs, h.m, h.n, h.count, joined, 8, 128, 64, 64, 24.6e3), st));
+    return from_hip(teal::launch_experts_mx4(h, experts_shape(pairs, h.m, h.n, h.count, joined, 32, 512, 512, 16, 92e3), st));
 }
 
 static teal::ExpertHostArgs experts_args(int count, const void *const *W, const void *const *scale,
