@@ -500,8 +500,9 @@ teal_status teal_sparse_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *
  *   the largest finite number; a v that is NaN comes last.
  *   0 <= tokens <= 2^24, 1 <= experts <= TEAL_MAX_EXPERTS (else TEAL_ERR_SHAPE);
  *   groups 1..64 divides experts, 1 <= top_groups <= groups, group_top 1 or 2,
- *   1 <= top_k <= TEAL_MAX_TOP_K and at most the experts of top_groups groups (else
- *   TEAL_ERR_UNSUPPORTED); scaling finite (else TEAL_ERR_THRESHOLD).
+ *   1 <= top_k <= TEAL_MAX_TOP_K and at most the experts of top_groups groups, score one
+ *   of the two (else TEAL_ERR_UNSUPPORTED); scaling finite (else TEAL_ERR_THRESHOLD).
+ *   idx and weight are fully overwritten; one launch, no workspace.
  *
  * teal_sparse_experts_{bf16,mx4}: y_k[b][j] = s_{t_k[e]}(x_b) W_k[e]^T with
  * e = idx[b][j], for count (1..4) matrices per expert that read the same state: gate

@@ -6,8 +6,6 @@
 // Scales are stored in tiles of 8 channels by 16 blocks, 128 bytes: what an output tile of 512 columns reads of
 // a channel's scales are 16 bytes, and a row of them would be a line that the tiles beside it, on other XCDs,
 // fetch too; of a tile of scales the line's other bytes belong to the next channels of the same block.
-#include <type_traits>
-
 #include "gemv_common.h"
 #include "gemv_experts.h"
 #include "gemv_mlp.h"

@@ -96,6 +96,25 @@ def test_pack_is_the_quantiser_and_unpack_its_values(T, m, n):
     assert torch.equal(back[:n * m].view(n, m), finite)
 
 
+@pytest.mark.parametrize("m,n", [(9, 64), (128, 128), (257, 544), (320, 96)])
+def test_layout_of_weights_that_begin_anywhere(T, m, n):
+    b = layout_weights(m, n, 5)
+    codes, scales = ti.quantize_mx4(b)
+    room = torch.zeros(n * m + 8, dtype=torch.int16, device="cuda")
+    q = torch.empty(m, n // 2, dtype=torch.uint8, device="cuda")
+    s = torch.empty(len(scales), dtype=torch.uint8, device="cuda")
+    for shift in range(4):
+        w = room[shift:shift + n * m]
+        w.copy_(dev(b).flatten())
+        T.check(T.teal_pack_mx4(w, q, s, m, n))
+        assert np.array_equal(q.cpu().numpy(), codes) and np.array_equal(s.cpu().numpy(), scales)
+        room.fill_(77)
+        T.check(T.teal_unpack_mx4(q, s, w, m, n))
+        got = w.view(torch.bfloat16).double().cpu().numpy().reshape(n, m)
+        assert np.array_equal(got, ti.mx4_values(codes, scales).T, equal_nan=True)
+        assert bool((room[:shift] == 77).all()) and bool((room[shift + n * m:] == 77).all())
+
+
 def test_unpack_every_scale_and_code(T):
     m, n = 256, 32
     codes = np.tile(np.arange(16, dtype=np.uint8) * 16 + np.arange(16, dtype=np.uint8)[::-1], (m, 1))
