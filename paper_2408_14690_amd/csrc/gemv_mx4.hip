@@ -389,9 +389,11 @@ hipError_t launch_experts_mx4(const ExpertHostArgs &h, const GemvShape &sh, hipS
 //
 // A thread block has 128 channels by 128 outputs, a wavefront one block of 32 outputs of all of them, a lane two
 // neighbouring channels: the 32 rows of W[n][m] are read (written) 256 bytes at a time, a block's 32 weights are in
-// one lane's registers, and the conversions of the hardware take and give two outputs at once.  Codes and scales
-// pass through LDS so that a channel's 64 bytes of codes and 4 scales travel together: 16 bytes and one byte per
-// lane and wavefront were four times the requests.
+// one lane's registers, and the conversions of the hardware take and give two outputs at once.  (8192 x 28672:
+// 105 us to mx4, 5.7 TB/s, and 85 us back, 7.0; turned through LDS two bytes at a time both together took 715.)  Codes
+// and scales pass through LDS so that a channel's 64 bytes of codes and 4 scales travel together: 16 bytes and one byte
+// per lane and wavefront were four times the requests.  Large weights are read with four channels to a lane, 512 bytes
+// of a row (8192 x 28672 111 -> 105 us; 4096 x 1024 would be 64 blocks instead of 256).
 constexpr int kMx4PackRows = 128, kMx4PackWaves = 4;
 
 // Two bf16 values of neighbouring channels; a row of W begins on an even address only.
@@ -404,9 +406,10 @@ typedef unsigned Mx4Pair __attribute__((aligned(2)));
 constexpr size_t kLastCache = (size_t)256 << 20;
 inline bool mx4_whole_lines(const void *W, int m) { return m % 64 == 0 && (reinterpret_cast<uintptr_t>(W) & 127) == 0; }
 
+template <int ROWS>
 struct Mx4PackTile {
-    u32x4 codes[kMx4PackRows][kMx4PackWaves + 1];     // one of padding: lanes two channels apart do not meet in a bank
-    unsigned char scale[kMx4PackRows][kMx4PackWaves];
+    u32x4 codes[ROWS][kMx4PackWaves + 1];             // one of padding: lanes two channels apart do not meet in a bank
+    unsigned char scale[ROWS][kMx4PackWaves];
 };
 
 // Codes of channels c and c + 64 of the tile, all four blocks: where thread `t` has its part of the LDS tile and of
@@ -418,41 +421,51 @@ __device__ __forceinline__ size_t mx4_scale_place(int i, int b, int n)
     return ((size_t)(i / 8) * mx4_scale_tiles(n) + b / 16) * kMx4TileBytes + i % 8 * 16 + b % 16;
 }
 
-template <bool PAST>
+template <bool PAST, int PAIRS>
 __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint16_t *__restrict__ W,
                                                                       uint8_t *__restrict__ Wq,
                                                                       uint8_t *__restrict__ scale, int m, int n,
                                                                       int tiles_m)
 {
-    __shared__ Mx4PackTile tile;
+    constexpr int CH = 2 * PAIRS, ROWS = 64 * CH;
+    typedef unsigned Load __attribute__((ext_vector_type(PAIRS), aligned(2)));
+    __shared__ Mx4PackTile<ROWS> tile;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i0 = blockIdx.x % tiles_m * kMx4PackRows, b0 = blockIdx.x / tiles_m * kMx4PackWaves;
-    const int i = i0 + 2 * lane, blocks = n / 32;
+    const int i0 = blockIdx.x % tiles_m * ROWS, b0 = blockIdx.x / tiles_m * kMx4PackWaves;
+    const int i = i0 + CH * lane, blocks = n / 32;
     if (b0 + w < blocks) {                                  // wavefront-uniform
-        unsigned v[32];                                     // channel i in the lower half, i + 1 in the upper
+        unsigned v[32][PAIRS];                              // the first channel of a pair in the lower half
         const uint16_t *first = W + (size_t)(b0 + w) * 32 * m;
-        if (i0 + kMx4PackRows <= m) {
+        if (i0 + ROWS <= m) {
 #pragma unroll
             for (int r = 0; r < 32; ++r) {
-                const Mx4Pair *p = reinterpret_cast<const Mx4Pair *>(first + (size_t)r * m + i);
-                v[r] = PAST ? __builtin_nontemporal_load(p) : *p;
+                const Load *p = reinterpret_cast<const Load *>(first + (size_t)r * m + i);
+                const Load x = PAST ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+                for (int c = 0; c < PAIRS; ++c) v[r][c] = x[c];
             }
         } else {
 #pragma unroll
-            for (int r = 0; r < 32; ++r) {
-                const uint16_t *p = first + (size_t)r * m + i;
-                v[r] = i + 1 < m ? *reinterpret_cast<const Mx4Pair *>(p) : i < m ? *p : 0u;
-            }
+            for (int r = 0; r < 32; ++r)
+#pragma unroll
+                for (int c = 0; c < PAIRS; ++c) {
+                    const uint16_t *p = first + (size_t)r * m + i + 2 * c;
+                    const int at = i + 2 * c;
+                    v[r][c] = at + 1 < m ? *reinterpret_cast<const Mx4Pair *>(p) : at < m ? *p : 0u;
+                }
         }
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-        u16x2 largest = {0, 0};
+        u16x2 largest[PAIRS] = {};
 #pragma unroll
         for (int r = 0; r < 32; ++r)
-            largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, v[r] & 0x7FFF7FFFu));
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < PAIRS; ++c)
+                largest[c] = __builtin_elementwise_max(largest[c], __builtin_bit_cast(u16x2, v[r][c] & 0x7FFF7FFFu));
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
             // floor(log2) of the largest magnitude; below 2^-125 the scale is the smallest one anyway
-            const int s = largest[c] >= 0x7F80u ? 255 : max((int)(largest[c] >> 7) - 2, 0);
+            const unsigned most = largest[c / 2][c % 2];
+            const int s = most >= 0x7F80u ? 255 : max((int)(most >> 7) - 2, 0);
             const float x = __uint_as_float((unsigned)s << 23);
             u32x4 codes = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -460,8 +473,8 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint
                 unsigned word = 0;
 #define TEAL_PAIR(B)                                                                           \
     do {                                                                                       \
-        const unsigned two = __builtin_amdgcn_perm(v[8 * q + 2 * B + 1], v[8 * q + 2 * B],     \
-                                                   c ? 0x07060302u : 0x05040100u);             \
+        const unsigned two = __builtin_amdgcn_perm(v[8 * q + 2 * B + 1][c / 2], v[8 * q + 2 * B][c / 2], \
+                                                   c % 2 ? 0x07060302u : 0x05040100u);         \
         word = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, __builtin_bit_cast(bf16x2, two), x, B); \
     } while (0)
                 TEAL_PAIR(0);
@@ -471,24 +484,25 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void pack_mx4_kernel(const uint
 #undef TEAL_PAIR
                 codes[q] = s == 255 ? 0u : word;
             }
-            tile.codes[2 * lane + c][w] = codes;
-            tile.scale[2 * lane + c][w] = i + c < m ? (unsigned char)s : 0;
+            tile.codes[CH * lane + c][w] = codes;
+            tile.scale[CH * lane + c][w] = i + c < m ? (unsigned char)s : 0;
         }
     } else {
-        tile.scale[2 * lane][w] = 0;
-        tile.scale[2 * lane + 1][w] = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) tile.scale[CH * lane + c][w] = 0;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < CH; ++k) {
         const int c = mx4_tile_channel(threadIdx.x, k), b = b0 + (int)threadIdx.x % kMx4PackWaves;
         if (i0 + c < m && b < blocks)
             *reinterpret_cast<u32x4 *>(Wq + ((size_t)(i0 + c) * blocks + b) * 16) =
                 tile.codes[c][threadIdx.x % kMx4PackWaves];
     }
     // zeros past the last channel and block of a tile of scales
+    static_assert(ROWS <= kMx4PackWaves * 64, "a thread per channel");
     const int c = threadIdx.x;
-    if (c < kMx4PackRows && i0 + c < (m + 7) / 8 * 8)
+    if (c < ROWS && i0 + c < (m + 7) / 8 * 8)
         for (int b = b0; b < (b0 + kMx4PackWaves < blocks ? b0 + kMx4PackWaves : mx4_scale_tiles(n) * 16);
              b += kMx4PackWaves)
             *reinterpret_cast<unsigned *>(scale + mx4_scale_place(i0 + c, b, n)) =
@@ -501,7 +515,7 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void unpack_mx4_kernel(const ui
                                                                         uint16_t *__restrict__ W, int m, int n,
                                                                         int tiles_m)
 {
-    __shared__ Mx4PackTile tile;
+    __shared__ Mx4PackTile<kMx4PackRows> tile;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i0 = blockIdx.x % tiles_m * kMx4PackRows, b0 = blockIdx.x / tiles_m * kMx4PackWaves;
     const int blocks = n / 32;
@@ -553,8 +567,8 @@ __global__ __launch_bounds__(kMx4PackWaves * 64) void unpack_mx4_kernel(const ui
 struct Mx4LayoutGrid {
     int tiles_m;
     long long tiles;
-    Mx4LayoutGrid(int m, int n)
-        : tiles_m((m + kMx4PackRows - 1) / kMx4PackRows),
+    Mx4LayoutGrid(int m, int n, int rows)
+        : tiles_m((m + rows - 1) / rows),
           tiles((long long)tiles_m * ((n / 32 + kMx4PackWaves - 1) / kMx4PackWaves))
     {
     }
@@ -562,17 +576,17 @@ struct Mx4LayoutGrid {
 
 hipError_t launch_pack_mx4(const void *W, uint8_t *Wq, uint8_t *scale, int m, int n, hipStream_t stream)
 {
-    const Mx4LayoutGrid g(m, n);
-    if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;      // more weights than a GPU has bytes
     const bool past = mx4_whole_lines(W, m) && (size_t)m * n * sizeof(uint16_t) > kLastCache;
-    hipLaunchKernelGGL(past ? pack_mx4_kernel<true> : pack_mx4_kernel<false>, dim3((unsigned)g.tiles),
+    const Mx4LayoutGrid g(m, n, past ? 2 * kMx4PackRows : kMx4PackRows);
+    if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;      // more weights than a GPU has bytes
+    hipLaunchKernelGGL((past ? pack_mx4_kernel<true, 2> : pack_mx4_kernel<false, 1>), dim3((unsigned)g.tiles),
                        dim3(kMx4PackWaves * 64), 0, stream, static_cast<const uint16_t *>(W), Wq, scale, m, n, g.tiles_m);
     return hipGetLastError();
 }
 
 hipError_t launch_unpack_mx4(const uint8_t *Wq, const uint8_t *scale, void *W, int m, int n, hipStream_t stream)
 {
-    const Mx4LayoutGrid g(m, n);
+    const Mx4LayoutGrid g(m, n, kMx4PackRows);
     if (g.tiles > 0x7fffffffLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL(mx4_whole_lines(W, m) ? unpack_mx4_kernel<true> : unpack_mx4_kernel<false>,
                        dim3((unsigned)g.tiles), dim3(kMx4PackWaves * 64), 0, stream, Wq, scale,
