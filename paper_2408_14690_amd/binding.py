@@ -1050,7 +1050,7 @@ def teal_sparse_experts_mx4_swiglu(Wq, scale, t, y, experts, idx, weight, tokens
     return _call(
         "teal_sparse_experts_mx4_swiglu",
         _ptr(Wq, experts * (m * n // 2), "Wq"), _ptr(scale, experts * _mx4_scale_need(m, n), "scale"),
-        _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _ptr(idx, 4 * pairs, "idx"),
+        _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _expert_numbers(idx, pairs),
         _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k), _ptr(gate, 4 * pairs * m, "gate"),
         _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream))

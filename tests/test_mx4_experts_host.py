@@ -184,3 +184,17 @@ def test_tensors_that_are_too_small_or_not_contiguous_are_refused():
         T.teal_route_experts(logits, None, 0, 4, 8, 1, 1, 1, 2, True, 1.0, idx.long(), weight, stream=0)
     with pytest.raises(ValueError):
         T.teal_sparse_gemv_mx4_multi([q, q], [s], [0.5, 0.5], [y, y], [64, 64], x, 64, WS, BIG, stream=0)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+def test_experts_down_refuses_64_bit_numbers(fmt):
+    torch = pytest.importorskip("torch")
+    weights, call = ((W, SC), T.teal_sparse_experts_mx4_swiglu) if fmt == "mx4" else ((W,), T.teal_sparse_experts_bf16_swiglu)
+    with pytest.raises(ValueError):
+        call(*weights, U, Y, 8, torch.zeros(2, 2, dtype=torch.int64), G, 2, 2, U, U, 64, 64, WS, BIG, stream=0)
+
+
+def test_a_threshold_beyond_32_bits_is_refused_by_the_call():
+    assert T.teal_sparse_gemv_mx4(W, SC, X, 1e39, Y, 64, 32, WS, BIG, stream=0) == T.TEAL_ERR_THRESHOLD
+    assert T.teal_sparse_gemv_mx4_multi([W, W], [SC, SC], [0.5, 1e39], [Y, Y], [32, 32], X, 64, WS, BIG,
+                                        stream=0) == T.TEAL_ERR_THRESHOLD
