@@ -3,14 +3,17 @@
 // The result is defined in binary64, but hardly a token needs all of its scores there.  fp32 values (the score and a
 // bias, or the logit), cut to the upper bits of a word above the expert's number, find top_k + 1 candidates, and
 // their binary64 scores, which are the weights, put those in order.  What the words left out matters only if a
-// third value lies within their error of the last one chosen: such tokens (one in 10^5 of ordinary ones) take a
-// wavefront each, by binary64 values throughout, and so do more than 512 experts or 15 of them chosen, and groups that do
-// not end with a lane's experts.  Groups whose fp32 values are too near each other are valued again in binary64.
+// third value lies within their error of the last one chosen: then the row goes on to 16 candidates, and tokens of more
+// equals than that take a wavefront each, by binary64 values throughout.  So do more than 512 experts or 15 of them chosen,
+// and groups that do not end with a lane's experts.  Groups whose fp32 values are too near each other are valued again by
+// the binary64 scores of their largest.
 //
-// What bounds it is instruction issue.  (us for 16384 tokens of 256 experts in 8 groups, 4 groups and 8 experts taken,
-// sigmoid scores and a bias; reading the logits takes 4: a wavefront per token in binary64 46; the selection on fp32
-// scores, the place of each maximum found by ballots, 28; a row of lanes per token on words, with all scores in
-// binary64, 24; fp32 scores and keys in sorted fours 16.)
+// What bounds it is instruction issue, 850 vector instructions of the four wavefronts a SIMD has, and the memory's and a
+// launch's latency.  (us for 16384 tokens of 256 experts in 8 groups, 4 groups and 8 experts taken, sigmoid scores and a
+// bias; reading the logits takes 4: a wavefront per token in binary64 46; the selection on fp32 scores, the place of each
+// maximum found by ballots, 28; a row of lanes per token on words, with all scores in binary64, 24; fp32 scores and keys
+// in sorted fours 16, 1270 instructions; without branches and double work 12.4; all of a near group's scores in binary64,
+// for one or two wavefronts of a launch, cost all the others' wait: the two largest 11.)
 #include <hip/hip_runtime.h>
 
 #include "teal_internal.h"
@@ -47,13 +50,6 @@ __device__ __forceinline__ float row_max(float v)
     v = fmaxf(v, row_rotate<4>(v));
     return fmaxf(v, row_rotate<8>(v));
 }
-__device__ __forceinline__ float row_min(float v)
-{
-    v = fminf(v, row_rotate<1>(v));
-    v = fminf(v, row_rotate<2>(v));
-    v = fminf(v, row_rotate<4>(v));
-    return fminf(v, row_rotate<8>(v));
-}
 template <int CTRL>
 __device__ __forceinline__ double lane_of(double v)
 {
@@ -86,19 +82,22 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
-// Order of floats as that of unsigned numbers, none of them zero; -0 and 0 are equal.
+// Order of numbers as that of unsigned ones, none of them zero; -0 comes before 0.
 __device__ __forceinline__ unsigned order_key(float v)
 {
-    const unsigned u = __float_as_uint(v + 0.f);
-    return u ^ ((int)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
+    const unsigned u = __float_as_uint(v);
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(unsigned key)
 {
     return __uint_as_float(key ^ ((int)key < 0 ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-// A logit as it counts: NaN as -infinity, +infinity as the largest finite number.
-__device__ __forceinline__ float clean_logit(float l) { return l != l ? -__builtin_inff() : fminf(l, 3.402823466e38f); }
+// A logit as it counts: NaN as -infinity, +infinity as the largest finite number; and -0 as 0.
+__device__ __forceinline__ float clean_logit(float l)
+{
+    return fminf(fmaxf(l + 0.f, -__builtin_inff()), 3.402823466e38f);
+}
 
 // exp(x) for x of at most 709.78 to a last place or two: x = k ln 2 + r, the Taylor polynomial of degree 12 at
 // |r| <= 0.347 (the next term is below 2^-52), times 2^k.
@@ -139,14 +138,14 @@ __device__ __forceinline__ double softmax_part(double z, double top)
     return z == -__builtin_inf() ? 0.0 : exponential(z - top);
 }
 
-// fp32 sigmoid from the hardware's exponential and reciprocal.  What a wrong last place of the argument, of at most
-// 88 log2 e where it matters, does to s is below s (1 - s) |l| 2^-23 < 2^-25; a few last places of numbers of at most 1
-// come on top.
+// fp32 sigmoid from the hardware's exponential and reciprocal, 1 / (1 + e), wrong by at most kScoreError.  Wrong last places of
+// the argument (of at most 88 log2 e where it matters), of e (2^-23 relative), of the sum and of the reciprocal do
+// s (1 - s) |l| 2^-23 < 2^-25, s (1 - s) 2^-23 <= 2^-25, 2^-24 and 2^-23 to s: together less than 2^-22.
 __device__ __forceinline__ float rough_sigmoid(float l)
 {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * l));
 }
-constexpr float kScoreError = 0x1p-20f;
+constexpr float kScoreError = 0x1p-22f;
 
 // One token by one wavefront, in binary64 throughout; lane l has experts l, l + 64, ...  `values`: LDS for E * 64.
 template <int E>
@@ -251,20 +250,24 @@ __device__ void route_exactly(const RouteHostArgs &h, int token, double *values)
     }
 }
 
-// The two largest values of a lane's experts, then of a group in its `lanes` lanes (a power of two up to 16).
-template <int E, class V>
-__device__ __forceinline__ void largest_two(const V (&v)[E], int lanes, V &first, V &second)
+// The two largest values of a lane's experts.
+template <int E>
+__device__ __forceinline__ void largest_two(const float (&v)[E], float &first, float &second)
 {
-    const auto larger = [](V a, V b) { return a > b ? a : b; };
-    const auto smaller = [](V a, V b) { return a > b ? b : a; };
     first = v[0];
     second = -__builtin_inff();
 #pragma unroll
     for (int j = 1; j < E; ++j) {
-        if constexpr (sizeof(V) == 4) second = __builtin_amdgcn_fmed3f(first, second, v[j]);
-        else second = larger(second, smaller(first, v[j]));
-        first = larger(first, v[j]);
+        second = __builtin_amdgcn_fmed3f(first, second, v[j]);
+        first = fmaxf(first, v[j]);
     }
+}
+// From the two largest of each lane those of a group in its `lanes` lanes (a power of two up to 16).
+template <class V>
+__device__ __forceinline__ void largest_two_of_group(int lanes, V &first, V &second)
+{
+    const auto larger = [](V a, V b) { return a > b ? a : b; };
+    const auto smaller = [](V a, V b) { return a > b ? b : a; };
     const auto merge = [&](V a, V b) {
         second = larger(smaller(first, a), larger(second, b));
         first = larger(first, a);
@@ -280,7 +283,7 @@ __device__ __forceinline__ void largest_two(const V (&v)[E], int lanes, V &first
 template <class V>
 __device__ __forceinline__ int groups_before(V value, int groups, int group_lanes)
 {
-    const int lane = threadIdx.x & 63, row = lane & 48, group = (lane & 15) / group_lanes;
+    const int lane = threadIdx.x & 63, row = lane & 48, group = (lane & 15) >> __builtin_ctz((unsigned)group_lanes);
     int before = 0;
 #pragma unroll 1
     for (int g = 0; g < groups; g += 4) {
@@ -288,7 +291,8 @@ __device__ __forceinline__ int groups_before(V value, int groups, int group_lane
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[u] = __shfl(value, row + min((g + u) * group_lanes, 15));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) before += g + u < groups && (x[u] > value || (x[u] == value && g + u < group));
+        for (int u = 0; u < 4; ++u)          // (not && and ||, which become branches)
+            before += (int)((g + u < groups) & ((x[u] > value) | ((x[u] == value) & (g + u < group))));
     }
     return before;
 }
@@ -339,7 +343,16 @@ __device__ __forceinline__ void remove_key(unsigned (&key)[E], unsigned taken)
 template <int E>
 __device__ __forceinline__ void lane_values(float (&v)[E], const float *p, int l16, int count, bool quads)
 {
-    if (E % 4 == 0 && quads) {
+    if (E % 4 == 0 && quads && count == 16 * E) {
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(p + l16 * E + j);
+            v[j] = q.x;
+            v[j + 1] = q.y;
+            v[j + 2] = q.z;
+            v[j + 3] = q.w;
+        }
+    } else if (E % 4 == 0 && quads) {
 #pragma unroll
         for (int j = 0; j < E; j += 4) {
             const float4 q = l16 * E + j < count ? *reinterpret_cast<const float4 *>(p + l16 * E + j)
@@ -375,16 +388,13 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
     const float *logits = h.logits + (size_t)token * h.experts;
     float l[E];
     lane_values(l, logits, l16, h.experts, quads);
-    float bias[E], error = 0.f;
+    float bias[E], error = 0.f;                          // of a bias that is infinite or NaN: not finite, nothing is sure
     if (biased) {
-        float largest = 0.f;
+        unsigned largest = 0;
         lane_values(bias, h.bias, l16, h.experts, quads);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            bias[j] = bias[j] != bias[j] ? -__builtin_inff() : bias[j];
-            largest = fmaxf(largest, fabsf(bias[j]));
-        }
-        error = 0x1p-23f * row_max(largest);             // (of an infinite one: nothing is sure)
+        for (int j = 0; j < E; ++j) largest = max(largest, __float_as_uint(bias[j]) & 0x7FFFFFFFu);
+        error = 0x1p-23f * __uint_as_float(row_max(largest));
     }
     if (scored) error += kScoreError + 0x1p-23f;         // of any value, twice what rounding a sum does
 #pragma unroll
@@ -414,100 +424,158 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
 #pragma unroll
         for (int j = 0; j < E; ++j) v[j] = rough_sigmoid(l[j]);
     }
+    if (biased) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-        if (biased) v[j] += bias[j];
-        else if (!two) v[j] = l[j];
+        for (int j = 0; j < E; ++j) v[j] += bias[j];                   // (no sum is -0: no score is)
+    } else if (!two) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = l[j];
+    }
+    if (!full) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = l16 * E + j < h.experts ? v[j] : -__builtin_inff();
+    }
+    bool taken = true, sure = error < __builtin_inff();
+    if (h.groups > 1) {
+        if (h.top_groups < h.groups) {
+            const bool sum_two = h.group_top == 2 && h.experts > h.groups;
+            float first, second;
+            largest_two(v, first, second);
+            const float lane_first = first, lane_second = second;
+            largest_two_of_group(group_lanes, first, second);
+            const float value = sum_two ? first + second : first;
+            // The largest value again and again.  It takes equal groups all at once, which their number tells.
+            unsigned left = order_key(value), in = 0;
+            taken = false;
+#pragma unroll 1
+            for (int g = 0; g < h.top_groups; ++g) {
+                in = row_max(left);
+                const bool here = left == in;
+                taken |= here;
+                left = here ? 0u : left;
+            }
+            // (row-uniform; two values of two scores each)
+            const bool equal = (int)__popc((unsigned)(__ballot(taken) >> row) & 0xFFFFu) != h.top_groups * group_lanes;
+            const bool near = equal || (scored && !(key_value(in) - key_value(row_max(left)) > 5.f * error));
+            if (__ballot(near)) {
+                bool before;
+                if (scored) {
+                    // In binary64 those of a lane's scores that count, if it is certain which: none of another value
+                    // within its error.
+                    const float least = (sum_two ? lane_second : lane_first) - 2.f * error;
+                    float l1 = 0.f, l2 = 0.f, b1 = 0.f, b2 = 0.f;
+                    int most = 0;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        l1 = v[j] == lane_first ? l[j] : l1;
+                        l2 = v[j] == lane_second ? l[j] : l2;
+                        most += v[j] >= least;
+                    }
+                    if (biased) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) {
+                            b1 = v[j] == lane_first ? bias[j] : b1;
+                            b2 = v[j] == lane_second ? bias[j] : b2;
+                        }
+                    }
+                    const auto score = [&](float l) {
+                        return h.sigmoid ? sigmoid_score((double)l) : softmax_part((double)l, top) * scale;
+                    };
+                    const bool none = lane_first == -__builtin_inff();             // a lane of no group
+                    double a = none ? -__builtin_inf() : score(l1) + (double)b1;
+                    double b = lane_second == -__builtin_inff() ? -__builtin_inf() : score(l2) + (double)b2;
+                    if (b > a) {
+                        const double c = a;
+                        a = b;
+                        b = c;
+                    }
+                    const bool certain = none || (most <= (sum_two ? 2 : 1) && !(sum_two && lane_first == lane_second));
+                    sure &= !(near && (unsigned)(__ballot(!certain) >> row) & 0xFFFFu);
+                    largest_two_of_group(group_lanes, a, b);
+                    before = groups_before(sum_two ? a + b : a, h.groups, group_lanes) < h.top_groups;
+                } else {
+                    before = groups_before(value, h.groups, group_lanes) < h.top_groups;
+                }
+                taken = near ? before : taken;
+            }
+        }
+        if (two && !biased) {                                          // the experts' order is that of the logits
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = l[j];
+        }
     }
     unsigned key[E];                                                   // never 0 but for what takes no part
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-        key[j] = (order_key(biased ? v[j] : l[j]) & ~kIndex) | (kIndex - (unsigned)(l16 * E + j));
+    for (int j = 0; j < E; ++j) {
+        key[j] = (order_key(v[j]) & ~kIndex) | (kIndex - (unsigned)(l16 * E + j));
+        key[j] = taken ? key[j] : 0u;
+    }
     if (!full) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            key[j] = l16 * E + j < h.experts ? key[j] : 0u;
-            v[j] = l16 * E + j < h.experts ? v[j] : -__builtin_inff();
-        }
+        for (int j = 0; j < E; ++j) key[j] = l16 * E + j < h.experts ? key[j] : 0u;
     }
-    if (h.groups > 1) {
-        const bool sum_two = h.group_top == 2 && h.experts > h.groups;
-        float first, second;
-        largest_two(v, group_lanes, first, second);
-        const float value = sum_two ? first + second : first;
-        const bool member = l16 / group_lanes < h.groups;
-        bool taken = groups_before(value, h.groups, group_lanes) < h.top_groups;
-        if (scored && h.top_groups < h.groups) {
-            const float in = row_min(taken && member ? value : __builtin_inff());
-            const float out = row_max(!taken && member ? value : -__builtin_inff());
-            // two values of two scores each
-            if (__ballot(!(in - out > 5.f * error))) {
-                double z[E], a, b;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    z[j] = h.sigmoid ? sigmoid_score((double)l[j]) : softmax_part((double)l[j], top) * scale;
-                    if (biased) z[j] += (double)bias[j];
-                    z[j] = full || l16 * E + j < h.experts ? z[j] : -__builtin_inf();
-                }
-                largest_two(z, group_lanes, a, b);
-                double exact = sum_two ? a + b : a;
-                exact = exact != exact ? -__builtin_inf() : exact;
-                taken = groups_before(exact, h.groups, group_lanes) < h.top_groups;
+
+    // The largest key of the token again and again; top_k + 1 of them, and the value of the next.  If that is not enough
+    // to be sure, all 16 that the row has lanes for.
+    unsigned candidate = 0;
+    int found = 0, wanted = h.top_k + 1, expert, rank;
+    bool lives;
+    double score;
+    unsigned long long unsure;
+    sort_fours(key);
+    for (;;) {
+#pragma unroll 1
+        for (; found < wanted; ++found) {
+            const unsigned best = row_max(largest_key(key));
+            candidate = l16 == found ? best : candidate;
+            remove_key(key, best);
+        }
+        const unsigned rest = row_max(largest_key(key));
+        lives = candidate != 0;
+        expert = lives ? (int)(kIndex - (candidate & kIndex)) : 0;
+        const float its_bias = biased ? h.bias[expert] : 0.f;
+        const float logit = clean_logit(logits[expert]);
+        score = h.sigmoid ? sigmoid_score((double)logit) : softmax_part((double)logit, top);
+        if (all_sums) score *= scale;
+        double order = biased ? score + (double)its_bias : (double)logit;
+        if (order != order || !lives) order = -__builtin_inf();
+        // They come in the order of their words: nearly always that of their values.
+        rank = l16;
+        const double next = __shfl(order, row + min(l16 + 1, 15));             // (by all lanes)
+        const int next_lives = __shfl((int)lives, row + min(l16 + 1, 15));
+        if (__ballot(l16 + 1 < wanted && next_lives && !(order > next))) {
+            rank = 0;
+            for (int c = 0; c < wanted; ++c) {
+                const double o = __shfl(order, row + c);
+                const int oe = __shfl(lives ? expert : kNone, row + c);
+                rank += oe != kNone && (o > order || (o == order && oe < expert));
             }
         }
-#pragma unroll
-        for (int j = 0; j < E; ++j) key[j] = taken ? key[j] : 0u;
-    }
-
-    // The largest key of the token again and again; top_k + 1 of them, and the value of the next.
-    unsigned candidate = 0, rest = 0;
-    sort_fours(key);
-#pragma unroll 1
-    for (int c = 0; c <= h.top_k + 1; ++c) {
-        rest = row_max(largest_key(key));
-        candidate = l16 == c ? rest : candidate;
-        remove_key(key, rest);
-    }
-
-    const bool lives = candidate != 0 && l16 <= h.top_k;
-    const int expert = lives ? (int)(kIndex - (candidate & kIndex)) : 0;
-    const float logit = clean_logit(logits[expert]);
-    double score = h.sigmoid ? sigmoid_score((double)logit) : softmax_part((double)logit, top);
-    if (all_sums) score *= scale;
-    double order = biased ? score + (double)h.bias[expert] : (double)logit;
-    if (order != order || !lives) order = -__builtin_inf();
-    // They come in the order of their words: nearly always that of their values.
-    int rank = l16;
-    const double next = __shfl(order, row + min(l16 + 1, 15));             // (by all lanes)
-    const int next_lives = __shfl((int)lives, row + min(l16 + 1, 15));
-    if (__ballot(l16 < h.top_k && next_lives && !(order > next))) {
-        rank = 0;
-        for (int c = 0; c <= h.top_k; ++c) {
-            const double o = __shfl(order, row + c);
-            const int oe = __shfl(lives ? expert : kNone, row + c);
-            rank += oe != kNone && (o > order || (o == order && oe < expert));
+        // The last one chosen has to be ahead of everything that is no candidate: the next word's value is at most this.
+        // (-infinity is what it is, and equal ones are in order.)
+        bool ahead = sure;
+        if (ahead && lives && rank == h.top_k - 1 && rest != 0) {
+            const float most = key_value(rest | kIndex);
+            ahead = order > (double)most + (biased ? (double)error : 0.0) || most == -__builtin_inff();
         }
-    }
-    // The last one chosen has to be ahead of everything that is no candidate: the next word's value is at most this.
-    // (-infinity is what it is, and equal ones are in order.)
-    bool sure = true;
-    if (lives && rank == h.top_k - 1 && rest != 0) {
-        const float most = key_value(rest | kIndex);
-        sure = order > (double)most + (biased ? (double)error : 0.0) || most == -__builtin_inff();
+        unsure = __ballot(!ahead);
+        if (!unsure || wanted == 16) break;
+        wanted = 16;
     }
     const bool chosen = lives && rank < h.top_k;
     if (h.renormalise) {
         const double total = row_sum(chosen ? score : 0.0);
         score = total > 0.0 ? score / total : 0.0;
     }
-    const unsigned long long unsure = __ballot(!sure);
     if (chosen && token0 + lane / 16 < h.tokens && !(unsure >> row & 0xFFFF)) {
         h.idx[(size_t)token * h.top_k + rank] = expert;
         h.weight[(size_t)token * h.top_k + rank] = (float)(score * (double)h.scaling);
     }
-    for (int c = 0; c < 4; ++c)
-        if (unsure >> 16 * c & 0xFFFF && token0 + c < h.tokens)
-            route_exactly<(E + 3) / 4>(h, token0 + c, values[w]);
+    if (unsure) {
+        for (int c = 0; c < 4; ++c)
+            if (unsure >> 16 * c & 0xFFFF && token0 + c < h.tokens)
+                route_exactly<(E + 3) / 4>(h, token0 + c, values[w]);
+    }
 }
 
 template <int E>

@@ -138,6 +138,22 @@ def test_route_of_scores_next_to_each_other(T, tokens, experts, groups, top_grou
         check_route(T, logits, b, sigmoid, groups, top_groups, group_top, top_k, True, 1.0)
 
 
+@pytest.mark.parametrize("experts,groups,top_groups,group_top,top_k", [(256, 8, 4, 2, 8), (64, 4, 1, 1, 4), (48, 3, 2, 2, 15), (16, 16, 7, 1, 5),
+                                                                      (32, 16, 5, 2, 6), (512, 8, 3, 2, 8)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_route_of_groups_next_to_each_other(T, experts, groups, top_groups, group_top, top_k, sigmoid):   # noqa: F811
+    """Groups of the same experts in other orders, whose largest differ by less than an fp32 score can tell, next to tokens
+    of ordinary groups."""
+    rng = np.random.default_rng(experts + groups)
+    tokens, size = 402, experts // groups
+    one = np.sort(rng.standard_normal((tokens, 1, size)), -1)
+    logits = rng.permuted(np.tile(one, (1, groups, 1)), axis=-1)
+    logits = (logits * (1 + 2e-7 * rng.standard_normal((tokens, groups, size)))).reshape(tokens, experts).astype(np.float32)
+    logits[1::3] = rng.standard_normal((len(logits[1::3]), experts))
+    for bias in (None, np.full(experts, 0.125, np.float32)):
+        check_route(T, logits, bias, sigmoid, groups, top_groups, group_top, top_k, True, 1.0)
+
+
 @pytest.mark.parametrize("experts,groups,top_groups,group_top,top_k", [(256, 8, 4, 2, 8), (128, 1, 1, 1, 8), (64, 8, 3, 1, 15),
                                                                       (60, 1, 1, 1, 4), (256, 1, 1, 1, 17), (512, 8, 2, 2, 6)])
 @pytest.mark.parametrize("sigmoid,biased", [(False, False), (False, True), (True, False), (True, True)])
