@@ -2,7 +2,7 @@
 // router chose, and their numbers are on the device.  A block reads the number of its expert and takes that
 // expert's matrix and threshold; it is otherwise a block of the products of one matrix (Body::run, gemv_mlp.h), so a
 // token's product with one expert is, up to the order of the sums, what the plain call gives on its matrix.
-// What bounds it is memory (us at 50 %: one token's two of eight 4096 -> 2 x 14336 bf16 experts 39.0, 6.0 TB/s), and for
+// What bounds it is memory (us at 50 %: one token's two of eight 4096 -> 2 x 14336 bf16 experts 39.5, 6.0 TB/s), and for
 // small experts what a block does before its first row: the number is there 0.5 us after its start, the threshold
 // 0.35 later (56 pairs of 2048 -> 2 x 768 mx4 in 13.8, their rows at 7.7 TB/s for 9.3 of them).  Asking for all
 // thresholds at once, and for the activations before the number, took 0.3 to 1 us longer.
