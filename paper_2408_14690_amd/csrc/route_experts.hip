@@ -4,8 +4,8 @@
 // bias, or the logit), cut to the upper bits of a word above the expert's number, find top_k + 1 candidates, and
 // their binary64 scores, which are the weights, put those in order.  What the words left out matters only if a
 // third value lies within their error of the last one chosen: then the row goes on to 16 candidates, and tokens of more
-// equals than that take a wavefront each, by binary64 values throughout.  So do more than 512 experts or 15 of them chosen,
-// and groups that do not end with a lane's experts.  Groups whose fp32 values are too near each other are valued again by
+// equals than that take a wavefront each, by binary64 values throughout.  So do more than 512 places for experts (a group has a
+// power of two), 15 of them chosen or 16 groups.  Groups whose fp32 values are too near each other are valued again by
 // the binary64 scores of their largest.
 //
 // What bounds it is instruction issue, 850 vector instructions of the four wavefronts a SIMD has, and the memory's and a
@@ -339,14 +339,14 @@ __device__ __forceinline__ void remove_key(unsigned (&key)[E], unsigned taken)
     }
 }
 
-// E values from place E * l16 on of the `count` at p, zeros past the end.  quads: by 16 bytes.
+// The `count` values from p on, zeros past them.  quads: by 16 bytes; full: E of them in all lanes.
 template <int E>
-__device__ __forceinline__ void lane_values(float (&v)[E], const float *p, int l16, int count, bool quads)
+__device__ __forceinline__ void lane_values(float (&v)[E], const float *p, int count, bool quads, bool full)
 {
-    if (E % 4 == 0 && quads && count == 16 * E) {
+    if (E % 4 == 0 && quads && full) {
 #pragma unroll
         for (int j = 0; j < E; j += 4) {
-            const float4 q = *reinterpret_cast<const float4 *>(p + l16 * E + j);
+            const float4 q = *reinterpret_cast<const float4 *>(p + j);
             v[j] = q.x;
             v[j + 1] = q.y;
             v[j + 2] = q.z;
@@ -355,8 +355,7 @@ __device__ __forceinline__ void lane_values(float (&v)[E], const float *p, int l
     } else if (E % 4 == 0 && quads) {
 #pragma unroll
         for (int j = 0; j < E; j += 4) {
-            const float4 q = l16 * E + j < count ? *reinterpret_cast<const float4 *>(p + l16 * E + j)
-                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 q = j < count ? *reinterpret_cast<const float4 *>(p + j) : make_float4(0.f, 0.f, 0.f, 0.f);
             v[j] = q.x;
             v[j + 1] = q.y;
             v[j + 2] = q.z;
@@ -364,34 +363,38 @@ __device__ __forceinline__ void lane_values(float (&v)[E], const float *p, int l
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = l16 * E + j < count ? p[l16 * E + j] : 0.f;
+        for (int j = 0; j < E; ++j) v[j] = j < count ? p[j] : 0.f;
     }
 }
 
-// A row of 16 lanes has a token, a lane of it experts E l .. E l + E - 1, and after the selection candidate l.
-// group_lanes: lanes of a group, a power of two up to 16.  quads: logits and bias begin on 16 bytes, and their number is
-// a multiple of four.
+// A row of 16 lanes has a token: place E l + j of a row is experts' value j of lane l, and after the selection lane l has
+// candidate l.  A group has group_lanes lanes, a power of two up to 16, the last of which may have fewer than E experts or
+// none; places increase with the experts' numbers.  quads: the logits and the bias of all lanes begin on 16 bytes, and
+// their numbers are multiples of four.
 template <int E>
 __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostArgs h, int group_lanes, bool quads)
 {
     __shared__ double values[kRouteWaves][E < 4 ? 64 : 16 * E];
-    constexpr unsigned kIndex = 16 * E - 1;    // the lower bits of a key: kIndex - expert, so that of equal values
+    constexpr unsigned kIndex = 16 * E - 1;    // the lower bits of a key: kIndex - place, so that of equal values
                                                // the lower number is the larger key
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int token0 = ((int)blockIdx.x * kRouteWaves + w) * 4;
     if (token0 >= h.tokens) return;            // no barrier below: a wavefront has its tokens to itself
     const int l16 = lane & 15, row = lane - l16, token = min(token0 + lane / 16, h.tokens - 1);
     const bool biased = h.bias != nullptr, full = h.experts == 16 * E;
+    const int group_shift = __builtin_ctz((unsigned)group_lanes), size = h.groups > 1 ? h.experts / h.groups : h.experts;
+    const int group = l16 >> group_shift, at = (l16 & (group_lanes - 1)) * E, first_expert = group * size + at;
+    const int count = group < h.groups ? min(max(size - at, 0), E) : 0;                  // of this lane
     const bool two = h.groups > 1 && h.group_top == 2;
     const bool scored = biased || two;                                  // all of them, not the candidates alone
     const bool all_sums = !h.sigmoid && (scored || !h.renormalise);
     const float *logits = h.logits + (size_t)token * h.experts;
     float l[E];
-    lane_values(l, logits, l16, h.experts, quads);
+    lane_values(l, logits + first_expert, count, quads, full);
     float bias[E], error = 0.f;                          // of a bias that is infinite or NaN: not finite, nothing is sure
     if (biased) {
         unsigned largest = 0;
-        lane_values(bias, h.bias, l16, h.experts, quads);
+        lane_values(bias, h.bias + first_expert, count, quads, full);
 #pragma unroll
         for (int j = 0; j < E; ++j) largest = max(largest, __float_as_uint(bias[j]) & 0x7FFFFFFFu);
         error = 0x1p-23f * __uint_as_float(row_max(largest));
@@ -401,7 +404,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
     for (int j = 0; j < E; ++j) l[j] = clean_logit(l[j]);
     if (!full) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) l[j] = l16 * E + j < h.experts ? l[j] : -__builtin_inff();
+        for (int j = 0; j < E; ++j) l[j] = j < count ? l[j] : -__builtin_inff();
     }
 
     double top = 0.0, scale = 1.0;
@@ -433,71 +436,70 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
     }
     if (!full) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = l16 * E + j < h.experts ? v[j] : -__builtin_inff();
+        for (int j = 0; j < E; ++j) v[j] = j < count ? v[j] : -__builtin_inff();
     }
     bool taken = true, sure = error < __builtin_inff();
     if (h.groups > 1) {
-        if (h.top_groups < h.groups) {
-            const bool sum_two = h.group_top == 2 && h.experts > h.groups;
-            float first, second;
-            largest_two(v, first, second);
-            const float lane_first = first, lane_second = second;
-            largest_two_of_group(group_lanes, first, second);
-            const float value = sum_two ? first + second : first;
-            // The largest value again and again.  It takes equal groups all at once, which their number tells.
-            unsigned left = order_key(value), in = 0;
-            taken = false;
+        const bool sum_two = h.group_top == 2 && h.experts > h.groups;
+        float first, second;
+        largest_two(v, first, second);
+        const float lane_first = first, lane_second = second;
+        largest_two_of_group(group_lanes, first, second);
+        const float value = sum_two ? first + second : first;
+        // The largest value again and again.  It takes equal groups all at once, which their number tells.
+        unsigned left = order_key(value), in = 0;
+        taken = false;
 #pragma unroll 1
-            for (int g = 0; g < h.top_groups; ++g) {
-                in = row_max(left);
-                const bool here = left == in;
-                taken |= here;
-                left = here ? 0u : left;
-            }
-            // (row-uniform; two values of two scores each)
-            const bool equal = (int)__popc((unsigned)(__ballot(taken) >> row) & 0xFFFFu) != h.top_groups * group_lanes;
-            const bool near = equal || (scored && !(key_value(in) - key_value(row_max(left)) > 5.f * error));
-            if (__ballot(near)) {
-                bool before;
-                if (scored) {
-                    // In binary64 those of a lane's scores that count, if it is certain which: none of another value
-                    // within its error.
-                    const float least = (sum_two ? lane_second : lane_first) - 2.f * error;
-                    float l1 = 0.f, l2 = 0.f, b1 = 0.f, b2 = 0.f;
-                    int most = 0;
+        for (int g = 0; g < h.top_groups; ++g) {
+            in = row_max(left);
+            const bool here = left == in;
+            taken |= here;
+            left = here ? 0u : left;
+        }
+        // (row-uniform; two values of two scores each)
+        const bool equal = (int)__popc((unsigned)(__ballot(taken) >> row) & 0xFFFFu) != h.top_groups * group_lanes;
+        const bool near = equal || (scored && !(key_value(in) - key_value(row_max(left)) > 5.f * error));
+        if (__ballot(near)) {
+            bool before;
+            if (scored) {
+                // In binary64 those of a lane's scores that count, if it is certain which: none of another value
+                // within its error.
+                const float last = sum_two && lane_second > -__builtin_inff() ? lane_second : lane_first;
+                const float least = last - 2.f * error;
+                float l1 = 0.f, l2 = 0.f, b1 = 0.f, b2 = 0.f;
+                int most = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    l1 = v[j] == lane_first ? l[j] : l1;
+                    l2 = v[j] == lane_second ? l[j] : l2;
+                    most += v[j] >= least;
+                }
+                if (biased) {
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
-                        l1 = v[j] == lane_first ? l[j] : l1;
-                        l2 = v[j] == lane_second ? l[j] : l2;
-                        most += v[j] >= least;
+                        b1 = v[j] == lane_first ? bias[j] : b1;
+                        b2 = v[j] == lane_second ? bias[j] : b2;
                     }
-                    if (biased) {
-#pragma unroll
-                        for (int j = 0; j < E; ++j) {
-                            b1 = v[j] == lane_first ? bias[j] : b1;
-                            b2 = v[j] == lane_second ? bias[j] : b2;
-                        }
-                    }
-                    const auto score = [&](float l) {
-                        return h.sigmoid ? sigmoid_score((double)l) : softmax_part((double)l, top) * scale;
-                    };
-                    const bool none = lane_first == -__builtin_inff();             // a lane of no group
-                    double a = none ? -__builtin_inf() : score(l1) + (double)b1;
-                    double b = lane_second == -__builtin_inff() ? -__builtin_inf() : score(l2) + (double)b2;
-                    if (b > a) {
-                        const double c = a;
-                        a = b;
-                        b = c;
-                    }
-                    const bool certain = none || (most <= (sum_two ? 2 : 1) && !(sum_two && lane_first == lane_second));
-                    sure &= !(near && (unsigned)(__ballot(!certain) >> row) & 0xFFFFu);
-                    largest_two_of_group(group_lanes, a, b);
-                    before = groups_before(sum_two ? a + b : a, h.groups, group_lanes) < h.top_groups;
-                } else {
-                    before = groups_before(value, h.groups, group_lanes) < h.top_groups;
                 }
-                taken = near ? before : taken;
+                const auto score = [&](float l) {
+                    return h.sigmoid ? sigmoid_score((double)l) : softmax_part((double)l, top) * scale;
+                };
+                const bool none = lane_first == -__builtin_inff();             // a lane of no group
+                double a = none ? -__builtin_inf() : score(l1) + (double)b1;
+                double b = lane_second == -__builtin_inff() ? -__builtin_inf() : score(l2) + (double)b2;
+                if (b > a) {
+                    const double c = a;
+                    a = b;
+                    b = c;
+                }
+                const bool certain = none || (most <= (sum_two ? 2 : 1) && !(sum_two && lane_first == lane_second));
+                sure &= !(near && (unsigned)(__ballot(!certain) >> row) & 0xFFFFu);
+                largest_two_of_group(group_lanes, a, b);
+                before = groups_before(sum_two ? a + b : a, h.groups, group_lanes) < h.top_groups;
+            } else {
+                before = groups_before(value, h.groups, group_lanes) < h.top_groups;
             }
+            taken = near ? before : taken;
         }
         if (two && !biased) {                                          // the experts' order is that of the logits
 #pragma unroll
@@ -512,7 +514,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
     }
     if (!full) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) key[j] = l16 * E + j < h.experts ? key[j] : 0u;
+        for (int j = 0; j < E; ++j) key[j] = j < count ? key[j] : 0u;
     }
 
     // The largest key of the token again and again; top_k + 1 of them, and the value of the next.  If that is not enough
@@ -532,7 +534,8 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
         }
         const unsigned rest = row_max(largest_key(key));
         lives = candidate != 0;
-        expert = lives ? (int)(kIndex - (candidate & kIndex)) : 0;
+        const int place = (int)(kIndex - (candidate & kIndex));
+        expert = lives ? place - (place / E >> group_shift) * (group_lanes * E - size) : 0;
         const float its_bias = biased ? h.bias[expert] : 0.f;
         const float logit = clean_logit(logits[expert]);
         score = h.sigmoid ? sigmoid_score((double)logit) : softmax_part((double)logit, top);
@@ -588,16 +591,17 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_exactly_kernel(RouteHo
 
 }  // namespace
 
-hipError_t launch_route_experts(const RouteHostArgs &h, hipStream_t stream)
+hipError_t launch_route_experts(const RouteHostArgs &args, hipStream_t stream)
 {
-    int per_lane = 1;                          // of a row
-    while (16 * per_lane < h.experts) per_lane *= 2;
-    const int size = h.experts / h.groups, lanes = size / per_lane;
-    const bool by_lanes = h.groups == 1 || (size % per_lane == 0 && (lanes & (lanes - 1)) == 0);
-    const int group_lanes = h.groups == 1 ? 16 : lanes;
+    RouteHostArgs h = args;
+    if (h.top_groups == h.groups) h.groups = h.top_groups = 1;      // all take part
+    const int size = h.experts / h.groups;
+    int group_lanes = 16, per_lane = 1;        // of a row
+    while (group_lanes * h.groups > 16) group_lanes /= 2;
+    while (group_lanes * per_lane < size && per_lane <= 32) per_lane *= 2;
     const dim3 block(kRouteWaves * 64);
-    if (by_lanes && per_lane <= 32 && h.top_k < 16) {
-        const bool quads = h.experts % 4 == 0 && (reinterpret_cast<uintptr_t>(h.logits) & 15) == 0 &&
+    if (group_lanes > 0 && per_lane <= 32 && h.top_k < 16) {
+        const bool quads = size % 4 == 0 && (reinterpret_cast<uintptr_t>(h.logits) & 15) == 0 &&
                            (reinterpret_cast<uintptr_t>(h.bias) & 15) == 0;
         const dim3 grid((unsigned)((h.tokens + 4 * kRouteWaves - 1) / (4 * kRouteWaves)));
 #define TEAL_ROUTE(E) hipLaunchKernelGGL(route_rows_kernel<E>, grid, block, 0, stream, h, group_lanes, quads)

@@ -166,6 +166,25 @@ def test_route_of_many_tokens(T, experts, groups, top_groups, group_top, top_k, 
     check_route(T, logits, bias, sigmoid, groups, top_groups, group_top, top_k, sigmoid, 2.5)
 
 
+@pytest.mark.parametrize("size,groups", [(11, 4), (11, 8), (3, 5), (1, 16), (2, 7), (17, 8), (33, 15), (128, 3), (129, 2), (32, 16), (20, 6),
+                                         (33, 16), (5, 17), (255, 4)])
+@pytest.mark.parametrize("sigmoid,biased", [(False, False), (False, True), (True, False), (True, True)])
+def test_route_of_groups_of_any_size(T, size, groups, sigmoid, biased):   # noqa: F811
+    rng = np.random.default_rng(100 * size + groups)
+    experts = size * groups
+    logits = rng.standard_normal((150, experts)).astype(np.float32)
+    logits[3, :size] = -np.inf                                 # groups with nothing in them
+    logits[4, size:] = -np.inf
+    logits[5] = 0.5
+    logits[6::10] = np.round(2 * logits[6::10]) / 2            # many equal ones
+    bias = (0.1 * rng.standard_normal(experts)).astype(np.float32) if biased else None
+    for top_groups in {1, groups // 2, groups - 1, groups}:
+        for group_top in (1, 2):
+            # the sum of two scores of a softmax over few equal logits is a matter of its rounding
+            rows = [r for r in range(150) if sigmoid or group_top == 1 or r not in range(6, 150, 10)]
+            check_route(T, logits[rows], bias, sigmoid, groups, top_groups, group_top, min(7, top_groups * size), True, 1.0)
+
+
 @pytest.mark.parametrize("experts,groups", [(64, 1), (400, 1), (256, 8), (15, 1), (48, 3)])
 def test_route_of_logits_that_begin_anywhere(T, experts, groups):   # noqa: F811
     rng = np.random.default_rng(experts)
