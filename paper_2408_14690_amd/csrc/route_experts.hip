@@ -8,7 +8,7 @@
 // power of two), 15 of them chosen or 16 groups.  Groups whose fp32 values are too near each other are valued again by
 // the binary64 scores of their largest.
 //
-// What bounds it is instruction issue, 850 vector instructions of the four wavefronts a SIMD has, and the memory's and a
+// What bounds it is instruction issue, 880 vector instructions of the four wavefronts a SIMD has, and the memory's and a
 // launch's latency.  (us for 16384 tokens of 256 experts in 8 groups, 4 groups and 8 experts taken, sigmoid scores and a
 // bias; reading the logits takes 4: a wavefront per token in binary64 46; the selection on fp32 scores, the place of each
 // maximum found by ballots, 28; a row of lanes per token on words, with all scores in binary64, 24; fp32 scores and keys
@@ -534,8 +534,8 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_rows_kernel(RouteHostA
         }
         const unsigned rest = row_max(largest_key(key));
         lives = candidate != 0;
-        const int place = (int)(kIndex - (candidate & kIndex));
-        expert = lives ? place - (place / E >> group_shift) * (group_lanes * E - size) : 0;
+        const unsigned place = kIndex - (candidate & kIndex);
+        expert = lives ? (int)(place - (place / E >> group_shift) * (unsigned)(group_lanes * E - size)) : 0;
         const float its_bias = biased ? h.bias[expert] : 0.f;
         const float logit = clean_logit(logits[expert]);
         score = h.sigmoid ? sigmoid_score((double)logit) : softmax_part((double)logit, top);
