@@ -512,7 +512,8 @@ teal_status teal_sparse_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *
  *          experts' matrices one behind the other, [experts][m][n_k] bf16, 16-byte
  *          aligned; Wq[k] [experts][m][n_k/2], scale[k] [experts] times
  *          teal_mx4_scale_bytes(m, n_k) bytes.  t[k]: DEVICE fp32 [experts]; it cannot
- *          be checked, and a negative or NaN threshold counts as 0.
+ *          be checked: a negative or NaN threshold counts as 0, and nothing is above
+ *          +infinity, not even an infinite input.
  *          y[k]: [tokens][top_k][n_k] fp32.
  *   idx    DEVICE int32 [tokens][top_k].  A number outside [0, experts) is no
  *          expert (a padded token): zeros.  The same expert may occur again.

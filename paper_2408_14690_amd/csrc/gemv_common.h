@@ -305,11 +305,12 @@ __device__ __forceinline__ void pairs_of_slice(float2 (&raw)[E], const float *a,
     }
 }
 
-// The largest fp16 value that is not above t (finite and >= 0: the entry points accept no other).  An fp16
-// magnitude is above t exactly if it is above this, so an fp16 state is compared as it is.
+// The largest fp16 value that is not above t (>= 0): t rounded towards zero, 65504 for a finite t beyond, infinity for
+// infinity, which only a threshold in device memory can be.  An fp16 magnitude is above t exactly if it is above this,
+// so an fp16 state is compared as it is.
 __device__ __forceinline__ _Float16 half_threshold(float t)
 {
-    return __builtin_bit_cast(_Float16, __builtin_amdgcn_cvt_pkrtz(fminf(t, 65504.f), 0.f)[0]);
+    return __builtin_bit_cast(_Float16, __builtin_amdgcn_cvt_pkrtz(t, 0.f)[0]);
 }
 
 // Where a block's activations come from.  A source loads what it needs for E channels of a slice that lie 64

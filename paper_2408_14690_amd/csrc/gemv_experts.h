@@ -28,8 +28,8 @@ struct ExpertArgs {
     Meeting meet;
 };
 
-// A threshold in device memory has not been checked: one that no call would accept counts as zero.  (A negative
-// one would keep the zeros past the end of a slice, more than the list has room for.)
+// A threshold in device memory has not been checked: a negative one or a NaN counts as zero.  (A negative one would keep
+// the zeros past the end of a slice, more than the list has room for.)  An infinite one stays: nothing is above it.
 __device__ __forceinline__ float expert_threshold(const float *t, int e) { return fmaxf(t[e], 0.f); }
 
 // Gate and up: y_k[pair] = s_{t_k[e]}(x[token]) W_k[e]^T, e = idx[pair], pair = token * top_k + slot.  A pair

@@ -1,0 +1,93 @@
+"""The experts' calls at the ends of their ranges: infinite thresholds and those beyond fp16.
+
+Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
+import numpy as np
+import pytest
+
+import teal_inputs as ti
+from test_gpu_experts import Experts, expert_workspace, product
+from test_gpu_mx4 import T, dev, workspace  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def whole_sum(x, t, values):
+    """The product term by term, infinities and NaN included."""
+    kept = np.abs(x.astype(np.float64)) > t
+    with np.errstate(invalid="ignore"):
+        return (x[kept].astype(np.float64)[:, None] * values[kept]).sum(0)
+
+
+INFINITE = [(1, 4, 70, 64), (2, 3, 1000, 96), (8, 8, 4200, 1536)]       # slices of every way of compaction
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("tokens,top_k,m,n", INFINITE)
+def test_nothing_is_above_an_infinite_threshold(T, fmt, tokens, top_k, m, n):   # noqa: F811
+    """Not even an infinite input, which every finite threshold keeps, also those beyond fp16."""
+    rng = np.random.default_rng(m)
+    t = np.array([np.inf, 7e4, 0.5, np.inf, 3e38], np.float32)
+    ex = Experts(fmt, 5, m, [n], m)
+    x = rng.standard_normal((tokens, m)).astype(np.float16)
+    x[0, 5], x[0, m - 1], x[0, 9], x[-1, 11] = np.inf, -np.inf, 65504, np.nan
+    idx = ((np.arange(tokens)[:, None] + np.arange(top_k)) % 5).astype(np.int32)
+    idx[0, -1] = 4                          # the infinite inputs with the largest finite threshold, too
+    y = torch.full((tokens, top_k, n), 7.0, device="cuda")
+    ex(T, [dev(t)], [y], dev(idx), dev(x), expert_workspace(T, m, n, tokens * top_k))
+    got = y.cpu().numpy()
+    for b in range(tokens):
+        for j in range(top_k):
+            e = idx[b, j]
+            if t[e] == np.inf or b and t[e] > 65504:
+                assert not got[b, j].any(), (b, j)
+            elif b == 0:
+                assert np.array_equal(got[b, j], whole_sum(x[b], t[e], ex.values[0][e]), equal_nan=True), (b, j)
+            else:
+                want, bound = product(x[b], t[e], ex.values[0][e])
+                assert np.all(np.abs(got[b, j] - want) <= bound), (b, j)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("tokens,top_k,m,n", INFINITE)
+def test_an_expert_with_an_infinite_threshold_adds_nothing(T, fmt, tokens, top_k, m, n):   # noqa: F811
+    """Also as a token's first expert, whose threshold the slices of the others are added by."""
+    rng = np.random.default_rng(n)
+    t = np.array([np.inf, 0.5, 0.25], np.float32)
+    ex = Experts(fmt, 3, m, [n], n)
+    idx = (np.arange(top_k) % 3 * np.ones((tokens, 1))).astype(np.int32)
+    idx[-1] = 0 if tokens > 1 else idx[-1]
+    gate, up = rng.uniform(0.5, 3, (tokens, top_k, m)).astype(np.float32), rng.standard_normal((tokens, top_k, m)).astype(np.float32)
+    up[idx == 0, 3] = np.inf
+    up[idx == 0, m - 1] = -np.inf
+    weight = rng.uniform(0.1, 1, (tokens, top_k)).astype(np.float32)
+    h = torch.empty(tokens, top_k, m, dtype=torch.float16, device="cuda")
+    T.check(T.teal_swiglu_f16(dev(gate), dev(up), h, h.numel()))
+    h = h.cpu().numpy()
+    assert np.isinf(h[idx == 0]).any() and np.isfinite(h[idx > 0]).all()
+    y = torch.full((tokens, n), 7.0, device="cuda")
+    ex.down(T, dev(t), y, dev(idx), dev(weight), dev(gate), dev(up), expert_workspace(T, m, n, tokens * top_k))
+    got = y.cpu().numpy().astype(np.float64)
+    for b in range(tokens):
+        want, bound, size = np.zeros(n), np.zeros(n), np.zeros(n)
+        for j in range(top_k):
+            if idx[b, j]:
+                one, off = product(h[b, j], t[idx[b, j]], ex.values[0][idx[b, j]])
+                want += weight[b, j] * one
+                bound += weight[b, j] * off
+                size += weight[b, j] * np.abs(h[b, j].astype(np.float64)) @ np.abs(ex.values[0][idx[b, j]])
+        assert np.all(np.abs(got[b] - want) <= bound + (top_k * 16 + 1) * 2.0 ** -24 * size), b
+    if tokens > 1:
+        assert not got[-1].any()
+
+
+@pytest.mark.parametrize("m,n", [(300, 96), (2048, 1024), (16384, 64)])
+def test_finite_thresholds_beyond_fp16_keep_infinite_inputs(T, m, n):   # noqa: F811
+    w = ti.weights_bf16(n, m, 3)
+    values = ti.bf16_bits_to_f32(w).T.astype(np.float64)
+    wt, x = dev(ti.to_input_channel_major(w)), ti.gaussian_x(m, 4)
+    x[7], x[m // 2], x[9] = 65504, -np.inf, np.nan
+    y, ws = torch.empty(n, device="cuda"), workspace(T, m, n)
+    for t in (65503.9, 65504.0, 65520.0, 1e5, 3.4e38):
+        T.check(T.teal_sparse_gemv_bf16(wt, dev(x), t, y, m, n, ws))
+        assert np.array_equal(y.cpu().numpy(), whole_sum(x, np.float32(t), values), equal_nan=True), t
