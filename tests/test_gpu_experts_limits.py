@@ -1,4 +1,5 @@
-"""The experts' calls at the ends of their ranges: infinite thresholds and those beyond fp16.
+"""The experts' calls at the ends of their ranges: infinite thresholds and those beyond fp16, sums of unusual size that are
+finite.
 
 Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
 import numpy as np
@@ -91,3 +92,38 @@ def test_finite_thresholds_beyond_fp16_keep_infinite_inputs(T, m, n):   # noqa: 
     for t in (65503.9, 65504.0, 65520.0, 1e5, 3.4e38):
         T.check(T.teal_sparse_gemv_bf16(wt, dev(x), t, y, m, n, ws))
         assert np.array_equal(y.cpu().numpy(), whole_sum(x, np.float32(t), values), equal_nan=True), t
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("tokens,top_k,m,n", [(8, 8, 4200, 1536), (1, 32, 640, 64), (1, 8, 20000, 64), (8, 32, 130, 1024), (2, 2, 2048, 512),
+                                              (3, 1, 9000, 2048)])
+def test_finite_sums_of_unusual_size(T, fmt, tokens, top_k, m, n):   # noqa: F811
+    """Every slice of every expert counts once where the sums take the way past the column words: their size is in the
+    router's weights, so that nothing is infinite."""
+    ex = Experts(fmt, 2, m, [n], 4)
+    rng = np.random.default_rng(6)
+    need = T.teal_workspace_bytes_experts(m, n, tokens * top_k)
+    room = torch.full((need + 4096,), 0xEE, dtype=torch.uint8, device="cuda")
+    ws = room[:need]
+    ws.zero_()
+    idx = rng.integers(0, 2, (tokens, top_k)).astype(np.int32)
+    for scale in (2.0 ** -30, 2.0 ** -14, 1.0, 2.0 ** 13, 2.0 ** 40):
+        gate, up = rng.standard_normal((2, tokens, top_k, m)).astype(np.float32)
+        weight = (scale * rng.uniform(0.5, 1, (tokens, top_k))).astype(np.float32)
+        h = torch.empty(tokens, top_k, m, dtype=torch.float16, device="cuda")
+        T.check(T.teal_swiglu_f16(dev(gate), dev(up), h, h.numel()))
+        h = h.cpu().numpy()
+        y = torch.empty(tokens, n, device="cuda")
+        ex.down(T, torch.zeros(2, device="cuda"), y, dev(idx), dev(weight), dev(gate), dev(up), ws)
+        for b in (0, tokens - 1):
+            want, bound, size = np.zeros(n), np.zeros(n), np.zeros(n)
+            for j in range(top_k):
+                one, off = product(h[b, j], 0, ex.values[0][idx[b, j]])
+                want += weight[b, j] * one
+                bound += weight[b, j] * off
+                size += weight[b, j] * np.abs(h[b, j].astype(np.float64)) @ np.abs(ex.values[0][idx[b, j]])
+            assert np.isfinite(want).all()
+            assert np.all(np.abs(y[b].cpu().numpy() - want) <= bound + (top_k * 16 + 1) * 2.0 ** -24 * size), (scale, b)
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xEE).all())
+    assert not bool(ws[:T.teal_survivors_offset()].any())
