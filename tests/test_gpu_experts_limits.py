@@ -1,12 +1,12 @@
-"""The experts' calls at the ends of their ranges: infinite thresholds and those beyond fp16, sums of unusual size that are
-finite.
+"""The experts' calls and the router at the ends of their ranges: infinite thresholds, sums of unusual size that are
+finite, groups of many equal scores.
 
 Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
 import numpy as np
 import pytest
 
 import teal_inputs as ti
-from test_gpu_experts import Experts, expert_workspace, product
+from test_gpu_experts import Experts, check_route, expert_workspace, product
 from test_gpu_mx4 import T, dev, workspace  # noqa: F401
 
 torch = pytest.importorskip("torch")
@@ -127,3 +127,19 @@ def test_finite_sums_of_unusual_size(T, fmt, tokens, top_k, m, n):   # noqa: F81
     torch.cuda.synchronize()
     assert bool((room[need:] == 0xEE).all())
     assert not bool(ws[:T.teal_survivors_offset()].any())
+
+
+@pytest.mark.parametrize("size,groups", [(11, 4), (11, 8), (3, 5), (1, 16), (2, 7), (17, 8), (33, 15), (128, 3), (129, 2), (32, 16), (20, 6),
+                                         (33, 16), (5, 17), (255, 4)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_softmax_groups_of_many_equal_scores(T, size, groups, biased):   # noqa: F811
+    """Groups valued by their two largest scores, of logits that are multiples of a half: equal logits have the same score,
+    so equal groups are equal and the lower number is taken."""
+    rng = np.random.default_rng(100 * size + groups)
+    experts = size * groups
+    logits = (np.round(2 * rng.standard_normal((60, experts))) / 2).astype(np.float32)
+    logits[5] = 0.5
+    bias = (0.1 * rng.standard_normal(experts)).astype(np.float32) if biased else None
+    for top_groups in {1, groups // 2, groups - 1, groups}:
+        for renormalise in (True, False):
+            check_route(T, logits, bias, False, groups, top_groups, 2, min(7, top_groups * size), renormalise, 1.0)
