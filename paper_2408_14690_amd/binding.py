@@ -283,6 +283,16 @@ def _find_current_stream():
 _current_stream = None
 
 
+def _forget_current_stream():
+    global _current_stream
+    _current_stream = None
+
+
+# A forked process asks torch again, which refuses: HIP does not survive a fork.
+if hasattr(os, "register_at_fork"):
+    os.register_at_fork(after_in_child=_forget_current_stream)
+
+
 def _stream(stream):
     if stream is None:
         global _current_stream
