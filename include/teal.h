@@ -497,7 +497,7 @@ teal_status teal_sparse_gemv_mx4_rmsnorm_multi(int count, const uint8_t *const *
  *          token's weights if renormalise != 0 (0 if that is 0), times scaling.
  *   Scores, v and sums are binary64; a weight is rounded once.  A NaN logit counts
  *   as -infinity, a logit of -infinity has the score 0, one of +infinity counts as
- *   the largest finite number; a v that is NaN comes last.
+ *   the largest finite number; a v that is NaN counts as -infinity.
  *   0 <= tokens <= 2^24, 1 <= experts <= TEAL_MAX_EXPERTS (else TEAL_ERR_SHAPE);
  *   groups 1..64 divides experts, 1 <= top_groups <= groups, group_top 1 or 2,
  *   1 <= top_k <= TEAL_MAX_TOP_K and at most the experts of top_groups groups, score one

@@ -1,5 +1,5 @@
 """The experts' calls and the router at the ends of their ranges: infinite thresholds, sums of unusual size that are
-finite, groups of many equal scores.
+finite, groups of many equal scores, sums that are no number.
 
 Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
 import numpy as np
@@ -143,3 +143,15 @@ def test_softmax_groups_of_many_equal_scores(T, size, groups, biased):   # noqa:
     for top_groups in {1, groups // 2, groups - 1, groups}:
         for renormalise in (True, False):
             check_route(T, logits, bias, False, groups, top_groups, 2, min(7, top_groups * size), renormalise, 1.0)
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+@pytest.mark.parametrize("experts,top_k", [(24, 12), (24, 24), (64, 15)])
+def test_sums_that_are_no_number_rank_as_the_lowest(T, experts, top_k, groups):   # noqa: F811
+    """NaN and -infinity among the biases are equal: by number, behind all others."""
+    rng = np.random.default_rng(experts)
+    logits = rng.standard_normal((9, experts)).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(experts)).astype(np.float32)
+    bias[1::3], bias[2::6] = np.nan, -np.inf
+    for top_groups, group_top in {(groups, 1), (max(1, groups // 2 + 1), 2)}:
+        check_route(T, logits, bias, True, groups, top_groups, group_top, min(top_k, experts // groups * top_groups), True, 1.0)
