@@ -454,8 +454,9 @@ teal_status teal_sparse_gemv_w4_multi(int count, const uint8_t *const *Wq,
  * Wq, scale in place of Wt_bf16; _multi, _swiglu and _rmsnorm_multi as the calls of
  * these names for the other formats (count 1..4; results of _swiglu and
  * _rmsnorm_multi are bitwise those of the producer call followed by
- * teal_sparse_gemv_mx4 or _multi).  Scale bytes of 253 and 254 are not supported (an
- * infinite weight may make its column NaN), weights below 2^-126 may count as zero.
+ * teal_sparse_gemv_mx4 or _multi).  Scale bytes of 253 and 254, which teal_pack_mx4
+ * never writes, are not supported: a weight beyond the range of bf16 may make the 8
+ * columns of its 4 bytes of Wq NaN.  Weights below 2^-126 may count as zero.
  */
 size_t teal_mx4_scale_bytes(int m, int n);
 teal_status teal_pack_mx4(const void *W_rowmajor, uint8_t *Wq, uint8_t *scale, int m, int n,

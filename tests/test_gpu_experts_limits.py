@@ -1,5 +1,5 @@
-"""The experts' calls and the router at the ends of their ranges: infinite thresholds, sums of unusual size that are
-finite, groups of many equal scores, sums that are no number.
+"""The experts' calls, the router and microscaled products at the ends of their ranges: infinite thresholds, sums of unusual
+size that are finite, groups of many equal scores, sums that are no number, infinite weights.
 
 Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
 import numpy as np
@@ -155,3 +155,22 @@ def test_sums_that_are_no_number_rank_as_the_lowest(T, experts, top_k, groups): 
     bias[1::3], bias[2::6] = np.nan, -np.inf
     for top_groups, group_top in {(groups, 1), (max(1, groups // 2 + 1), 2)}:
         check_route(T, logits, bias, True, groups, top_groups, group_top, min(top_k, experts // groups * top_groups), True, 1.0)
+
+
+@pytest.mark.parametrize("scale", [253, 254])
+def test_how_far_an_infinite_weight_reaches(T, scale):   # noqa: F811
+    m, n = 520, 96
+    codes, scales, x = *ti.random_mx4(m, n, 1), ti.gaussian_x(m, 2)
+    x[100], x[101] = 3, 0
+    for channel in (100, 101):
+        marked, levels = scales.copy(), codes.copy()
+        marked[ti.mx4_scale_places(m, n)[channel, 1]] = scale
+        levels[channel, 16:32] = 0x11                        # columns 32 to 63: a half
+        levels[channel, 16 + 5] = 0x17                       # column 42: six of a scale that makes it infinite
+        values = ti.mx4_values(levels, marked)
+        y = torch.empty(n, device="cuda")
+        T.check(T.teal_sparse_gemv_mx4(dev(levels), dev(marked), dev(x), 0.5, y, m, n, workspace(T, m, n)))
+        want, bound = product(x, 0.5, values)
+        beside = (np.arange(n) < 40) | (np.arange(n) >= 48) if channel == 100 else np.ones(n, bool)
+        with np.errstate(invalid="ignore"):
+            assert np.all(np.abs(y.cpu().numpy() - want)[beside] <= bound[beside])
