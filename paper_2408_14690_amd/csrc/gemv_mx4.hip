@@ -412,8 +412,8 @@ struct Mx4PackTile {
     unsigned char scale[ROWS][kMx4PackWaves];
 };
 
-// Codes of channels c and c + 64 of the tile, all four blocks: where thread `t` has its part of the LDS tile and of
-// memory, for pass k of 2.
+// The channel of the tile whose codes thread `t` moves between LDS and memory in pass k: 64 channels a pass, four threads to
+// a channel, a block each.  (Two passes for tiles of 128 channels, four for the wide ones of pack_mx4_kernel.)
 __device__ __forceinline__ int mx4_tile_channel(int t, int k) { return k * 64 + t / kMx4PackWaves; }
 
 __device__ __forceinline__ size_t mx4_scale_place(int i, int b, int n)

@@ -4,9 +4,9 @@
 // bias, or the logit), cut to the upper bits of a word above the expert's number, find top_k + 1 candidates, and
 // their binary64 scores, which are the weights, put those in order.  What the words left out matters only if a
 // third value lies within their error of the last one chosen: then the row goes on to 16 candidates, and tokens of more
-// equals than that take a wavefront each, by binary64 values throughout.  So do more than 512 places for experts (a group has a
-// power of two), 15 of them chosen or 16 groups.  Groups whose fp32 values are too near each other are valued again by
-// the binary64 scores of their largest.
+// equals than that take a wavefront each, by binary64 values throughout.  So do calls with more than 512 places for experts
+// (a group has a power of two), with more than 15 experts chosen or with more than 16 groups.  Groups whose fp32 values are
+// too near each other are valued again by the binary64 scores of their largest.
 //
 // What bounds it is instruction issue, 880 vector instructions of the four wavefronts a SIMD has, and the memory's and a
 // launch's latency.  (us for 16384 tokens of 256 experts in 8 groups, 4 groups and 8 experts taken, sigmoid scores and a

@@ -208,12 +208,16 @@ GemvShape mx4_shape(int m, const int *n, int count)
 // slices: bf16, 8 experts of 1024 -> 2048 joined 256 x 4 8.1, 128 x 2 6.9; 2 of 14336 -> 4096 512 x 8 26.3, 256 x 8
 // 22.0, 128 x 4 23.1; 2 pairs of 4096 -> 2 x 14336 512 x 1 55.8, x 2 40.6, x 4 42.8; mx4, 2 of 14336 -> 4096 joined in
 // 8 slices 13.7, 16 10.8; 8 pairs of 2048 -> 2 x 1024 in 4 7.0, 8 6.2.)  With more than one slice all blocks are
-// resident at once.  Tiles have from min_cols to all of max_lanes' columns in steps of whole lines: with 192 bytes of a
-// row, mx4 experts of 768 columns, neighbours fetch a line twice (56 pairs of 2048 -> 2 x 768 in 384 columns 16.2, in
-// 512, the second of a matrix half empty, 15.1).
+// resident at once, unless the input is longer than one slice may be.  Tiles have from min_cols to all of max_lanes'
+// columns in steps of whole lines: with 192 bytes of a row, mx4 experts of 768 columns, neighbours fetch a line twice
+// (56 pairs of 2048 -> 2 x 768 in 384 columns 16.2, in 512, the second of a matrix half empty, 15.1).  The fullest unit
+// is taken to have full tiles only, and every pair to have an expert: the host does not know which have none.
 GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, int elems_per_lane, int min_cols,
                         int step, int max_lanes, double rate)
 {
+    static_assert(teal::kMaxDim / 128 + teal::kMaxMatrices * teal::kMaxBatch * teal::kMaxTopK <=
+                      (int)(teal::kCounterBytes / sizeof(int)),
+                  "a counter per tile: kMaxDim columns of all pairs in tiles of 128 and more, one of a matrix part-empty");
     double best = -1.0;
     GemvShape sh{16, 1, 16 * elems_per_lane, 8, 4};
     double weights = 0.0;
@@ -228,7 +232,6 @@ GemvShape experts_shape(int copies, int m, const int *n, int count, int joined, 
             if (ks > teal::kMaxSlice) continue;
             const int s = (m + ks - 1) / ks;
             const long long blocks = tiles * s * copies;
-            if (s * joined > 1 && tiles * copies > (long long)(teal::kCounterBytes / sizeof(int))) continue;
             if (s > 1 && blocks > kComputeUnits && m <= teal::kMaxSlice) continue;
             const long long rounds = (blocks + kComputeUnits - 1) / kComputeUnits;
             double all = weights / kComputeUnits / rate;
