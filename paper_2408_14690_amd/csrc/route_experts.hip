@@ -99,7 +99,7 @@ __device__ __forceinline__ float clean_logit(float l)
     return fminf(fmaxf(l + 0.f, -__builtin_inff()), 3.402823466e38f);
 }
 
-// exp(x) for x of at most 709.78 to a last place or two: x = k ln 2 + r, the Taylor polynomial of degree 12 at
+// exp(x) for x of at most 709.7827 to a last place or two: x = k ln 2 + r, the Taylor polynomial of degree 12 at
 // |r| <= 0.347 (the next term is below 2^-52), times 2^k.
 __device__ __forceinline__ double exponential(double x)
 {
@@ -129,9 +129,10 @@ __device__ __forceinline__ double reciprocal(double d)
     r = fma(r, fma(-d, r, 1.0), r);
     return fma(r, fma(-d, r, 1.0), r);
 }
+// (-709.7827 lies between the last fp32 number whose exponential binary64 holds and the next.)
 __device__ __forceinline__ double sigmoid_score(double z)
 {
-    return z < -709.78 ? 0.0 : reciprocal(1.0 + exponential(-fmax(z, -709.78)));
+    return z < -709.7827 ? 0.0 : reciprocal(1.0 + exponential(-fmax(z, -709.7827)));
 }
 __device__ __forceinline__ double softmax_part(double z, double top)
 {

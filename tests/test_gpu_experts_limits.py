@@ -157,6 +157,21 @@ def test_sums_that_are_no_number_rank_as_the_lowest(T, experts, top_k, groups): 
         check_route(T, logits, bias, True, groups, top_groups, group_top, min(top_k, experts // groups * top_groups), True, 1.0)
 
 
+@pytest.mark.parametrize("experts,top_k", [(8, 3), (64, 6), (64, 16)])
+def test_sigmoid_scores_up_to_the_last_that_is_not_zero(T, experts, top_k):   # noqa: F811
+    """Renormalised scores of logits down to where exp(-l) leaves binary64, fp32 number by fp32 number at the end."""
+    last = np.float32(-709.78265)
+    assert np.isfinite(np.exp(-np.float64(last))) and np.exp(709.0) < np.exp(-np.float64(last))
+    with np.errstate(over="ignore"):
+        assert np.isinf(np.exp(-np.float64(np.nextafter(last, np.float32(-800)))))
+    steps = np.arange(-8, 60, dtype=np.float32) * np.float32(2.0 ** -14)
+    logits = np.full((len(steps), experts), -800, np.float32)
+    logits[:, ::3] = last + steps[:, None]
+    logits[::2, 1] = last
+    for bias in (None, np.zeros(experts, np.float32)):
+        check_route(T, logits, bias, True, 1, 1, 1, top_k, True, 1.0)
+
+
 @pytest.mark.parametrize("scale", [253, 254])
 def test_how_far_an_infinite_weight_reaches(T, scale):   # noqa: F811
     m, n = 520, 96
