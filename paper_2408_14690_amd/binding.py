@@ -1011,10 +1011,16 @@ def _expert_numbers(idx, pairs):
     return _ptr(idx, 4 * pairs, "idx")
 
 
+def _expert_floats(a, count, what):
+    if getattr(a, "element_size", None) is not None and a.element_size() == 8:
+        raise ValueError(f"{what}: 32-bit floats in device memory")             # (numpy's are 64-bit ones)
+    return _ptr(a, 4 * count, what)
+
+
 def _expert_thresholds(t_list, count, experts):
     if len(t_list) != count:
         raise ValueError("per-matrix lists must have the same length")
-    return _pointers([_ptr(t, 4 * experts, "t") or 0 for t in t_list])
+    return _pointers([_expert_floats(t, experts, "t") or 0 for t in t_list])
 
 
 def teal_sparse_experts_bf16(Wt_list, t_list, y_list, n_list, experts, idx, tokens, top_k, X_f16, m, workspace,
@@ -1048,8 +1054,8 @@ def teal_sparse_experts_bf16_swiglu(Wt_bf16, t, y, experts, idx, weight, tokens,
     pairs = tokens * top_k
     return _call(
         "teal_sparse_experts_bf16_swiglu",
-        _ptr(Wt_bf16, 2 * experts * m * n, "Wt"), _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"),
-        int(experts), _expert_numbers(idx, pairs), _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k),
+        _ptr(Wt_bf16, 2 * experts * m * n, "Wt"), _expert_floats(t, experts, "t"), _ptr(y, 4 * tokens * n, "y"),
+        int(experts), _expert_numbers(idx, pairs), _expert_floats(weight, pairs, "weight"), int(tokens), int(top_k),
         _ptr(gate, 4 * pairs * m, "gate"), _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace),
         _nbytes(workspace, workspace_bytes), _stream(stream))
 
@@ -1060,7 +1066,7 @@ def teal_sparse_experts_mx4_swiglu(Wq, scale, t, y, experts, idx, weight, tokens
     return _call(
         "teal_sparse_experts_mx4_swiglu",
         _ptr(Wq, experts * (m * n // 2), "Wq"), _ptr(scale, experts * _mx4_scale_need(m, n), "scale"),
-        _ptr(t, 4 * experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _expert_numbers(idx, pairs),
-        _ptr(weight, 4 * pairs, "weight"), int(tokens), int(top_k), _ptr(gate, 4 * pairs * m, "gate"),
+        _expert_floats(t, experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _expert_numbers(idx, pairs),
+        _expert_floats(weight, pairs, "weight"), int(tokens), int(top_k), _ptr(gate, 4 * pairs * m, "gate"),
         _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream))
