@@ -508,7 +508,7 @@ const char *teal_status_string(teal_status s)
     return "unknown status";
 }
 
-int teal_version(void) { return 418; }
+int teal_version(void) { return 419; }
 
 size_t teal_survivors_offset(void) { return teal::kCounterBytes; }
 
