@@ -2,10 +2,13 @@
 // router chose, and their numbers are on the device.  A block reads the number of its expert and takes that
 // expert's matrix and threshold; it is otherwise a block of the products of one matrix (Body::run, gemv_mlp.h), so a
 // token's product with one expert is, up to the order of the sums, what the plain call gives on its matrix.
-// What bounds it is memory (us at 50 %: one token's two of eight 4096 -> 2 x 14336 bf16 experts 39.5, 6.0 TB/s), and for
-// small experts what a block does before its first row: the number is there 0.5 us after its start, the threshold
-// 0.35 later (56 pairs of 2048 -> 2 x 768 mx4 in 13.8, their rows at 7.7 TB/s for 9.3 of them).  Asking for all
+// What bounds it is memory (us at 50 %: one token's two of eight 4096 -> 2 x 14336 bf16 experts 39.5 to 41.5, 5.7 to 6.0
+// TB/s), and for small experts the fullest unit and what a block does before its first row: the number is there 0.5 us after
+// its start, the threshold 0.35 later (56 pairs of 2048 -> 2 x 768 mx4 in 13.9, 9.3 of them from the first row to the last,
+// 46.8 MB at 5.0 TB/s: blocks of 512 columns beside blocks of 256, which end before them).  Asking for all
 // thresholds at once, and for the activations before the number, took 0.3 to 1 us longer.
+// Pairs are products of their own, in the tokens' order: an expert that several tokens chose is read for each of them
+// (8 tokens, 8 of 8 bf16 experts of 4096 -> 2 x 14336: 7.57 GB fetched in 1155, where the union of the rows is 1.87 GB).
 #pragma once
 
 #include "gemv_common.h"
