@@ -1,5 +1,5 @@
 """The experts' calls, the router and microscaled products at the ends of their ranges: infinite thresholds, sums of unusual
-size that are finite, groups of many equal scores, sums that are no number, infinite weights.
+size that are finite, groups of many equal scores, sums that are no number, infinite weights, the longest inputs.
 
 Tolerances of products as in test_gpu_mx4.py and test_gpu_experts.py."""
 import numpy as np
@@ -189,3 +189,55 @@ def test_how_far_an_infinite_weight_reaches(T, scale):   # noqa: F811
         beside = (np.arange(n) < 40) | (np.arange(n) >= 48) if channel == 100 else np.ones(n, bool)
         with np.errstate(invalid="ignore"):
             assert np.all(np.abs(y.cpu().numpy() - want)[beside] <= bound[beside])
+
+
+@pytest.mark.parametrize("fmt,n", [("bf16", 8), ("mx4", 32)])
+def test_the_longest_inputs(T, fmt, n):   # noqa: F811
+    """2^24 channels, 4096 slices, of which a few survive: the sum is what their roundings leave of it."""
+    m, rng = 1 << 24, np.random.default_rng(n)
+    rows = np.unique(np.concatenate([[0, 1, 4095, 4096, m - 4097, m - 4096, m - 2, m - 1], rng.integers(0, m, 40)]))
+    at = dev(rows)
+    x = np.zeros(m, np.float16)
+    x[rows] = rng.uniform(0.5, 2, len(rows))
+    if fmt == "mx4":
+        codes = rng.integers(0, 256, (len(rows), n // 2), dtype=np.uint8)
+        q = torch.zeros(1, m, n // 2, dtype=torch.uint8, device="cuda")
+        q[0, at] = dev(codes)
+        s = torch.full((T.teal_mx4_scale_bytes(m, n),), 120, dtype=torch.uint8, device="cuda")
+        values = ti.mx4_values(codes, np.full(ti.mx4_scale_bytes(len(rows), n), 120, np.uint8))
+        args = (q, s)
+    else:
+        w = torch.zeros(1, m, n, dtype=torch.bfloat16, device="cuda")
+        w[0, at] = dev(rng.standard_normal((len(rows), n)).astype(np.float32)).bfloat16()
+        values = w[0, at].double().cpu().numpy()
+        args = (w,)
+    ex = Experts(fmt, 1, 32, [32], 0)                        # for its calls, not for its weights
+    ex.m, ex.widths, ex.args = m, [n], [args]
+    t, ws = torch.full((1,), 0.25, device="cuda"), expert_workspace(T, m, n, 2)
+    idx, y = dev(np.array([[0, -1]], np.int32)), torch.full((1, 2, n), 7.0, device="cuda")
+    ex(T, [t], [y], idx, dev(x[None]), ws)
+    want, bound = product(x[rows], 0.25, values)
+    assert np.all(np.abs(y[0, 0].cpu().numpy() - want) <= bound) and not y[0, 1].any()
+    gate, up = torch.full((2, m), 80.0, device="cuda"), dev(x.astype(np.float32) / 80).repeat(2, 1)
+    h = torch.empty(m, dtype=torch.float16, device="cuda")
+    T.check(T.teal_swiglu_f16(gate, up, h, m))
+    h, z = h.cpu().numpy(), torch.full((1, n), 7.0, device="cuda")
+    ex.down(T, t, z, idx, torch.full((1, 2), 0.5, device="cuda"), gate, up, ws)
+    want, bound = product(h[rows], 0.25, values)
+    assert np.all(np.abs(z[0].cpu().numpy() - 0.5 * want) <= 0.5 * bound)
+    if fmt == "mx4":
+        y1 = torch.empty(n, device="cuda")
+        T.check(T.teal_sparse_gemv_mx4(q, s, dev(x), 0.25, y1, m, n, workspace(T, m, n)))
+        want, bound = product(x[rows], 0.25, values)
+        assert np.all(np.abs(y1.cpu().numpy() - want) <= bound)
+
+
+def test_the_most_tokens_of_a_router(T):   # noqa: F811
+    tokens = 1 << 24
+    logits = torch.randn(tokens, 4, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    idx, weight = torch.empty(tokens, 2, dtype=torch.int32, device="cuda"), torch.empty(tokens, 2, device="cuda")
+    T.check(T.teal_route_experts(logits, None, 1, tokens, 4, 1, 1, 1, 2, False, 1.0, idx, weight))
+    best = logits.sort(dim=1, descending=True, stable=True)
+    assert torch.equal(idx.long(), best.indices[:, :2])
+    score = torch.sigmoid(best.values[:, :2].double())
+    assert bool(((weight - score).abs() <= score * (2.0 ** -24 + 2.0 ** -48)).all())
