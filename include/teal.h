@@ -562,6 +562,106 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
                                            void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Many rows: a prompt, or a batch beyond TEAL_MAX_BATCH sequences, on the weights as the calls above store them.  Every row
+ * is a hidden state of its own.  Dense but for the threshold of teal_quantize_rows: what many rows keep together is
+ * every channel, so nothing is left to skip (Section 5.4.3 discusses a prompt's first half for its accuracy).
+ *
+ * 8-bit weights (Section 5.3), W[j][i] = Wq[i][j] * scale[j] as for teal_sparse_gemv_w8: rows to 8-bit integers with a
+ * scale each, and products of integers.
+ *
+ * teal_quantize_rows: for each row, v = s_t(x) (Definition 1), a = max |v_i|,
+ *     row_scale = a / 127 in binary32,  q_i = the integer nearest to 127 v_i / a, ties to even (0 if a is 0).
+ *   The quotient counts as a real number: no rounding of it decides q.  A NaN is dropped; an infinity makes
+ *   row_scale infinite and q_i = +-127 there and 0 elsewhere.
+ *   X [rows][m] of type TEAL_F16 or TEAL_BF16 (else TEAL_ERR_UNSUPPORTED), 2-byte aligned.  t as for every call.
+ *   Q [rows][teal_quantized_pitch(m)] int8, 16-byte aligned: rows of whole 128-byte lines, zeros behind channel m.
+ *   row_scale [rows] fp32.
+ *   0 <= rows <= TEAL_MAX_ROWS, 1 <= m <= TEAL_MAX_ROW_SUM (127 * 128 * 2^17 is below 2^31).
+ * teal_quantized_pitch: m rounded up to a multiple of 128; 0 if m is out of range.
+ * teal_quantize_rows_swiglu: the same of h = fp16(SiLU(gate) * up) in the arithmetic stated for
+ *   teal_sparse_gemv_bf16_swiglu; gate, up [rows][m] fp32, 4-byte aligned.
+ *
+ * teal_gemm_w8: Y[b][j] = binary32(binary32(binary32(S) * row_scale[b]) * scale[j]), S = sum_i Q[b][i] Wq[i][j], a whole
+ * number, exact.  teal_gemm_w8_multi: count (1..4) matrices that read the same rows, in one launch.
+ *   Wq, scale_f16, n   as for teal_sparse_gemv_w8 (_multi: HOST arrays of length count); n % 16 == 0.
+ *   Q, row_scale, rows, m  as teal_quantize_rows leaves them (Q 16-byte aligned; entries of -128 and anything but
+ *           zeros behind channel m are the caller's mistake: sums may then be wrong).
+ *   Y       [rows][n] fp32, 4-byte aligned, fully overwritten.
+ *   workspace  at least teal_workspace_bytes_gemm_w8(rows, m, n_0 + ... + n_{count-1}) bytes, zero before first use
+ *           like every workspace.  No survivor counts.
+ *   TEAL_ERR_SHAPE also where rows and widths make more blocks than one launch has (2^22 tiles of 32 x 128).
+ */
+#define TEAL_F16 0
+#define TEAL_BF16 1
+#define TEAL_MAX_ROWS 1048576
+#define TEAL_MAX_ROW_SUM 131072
+int teal_quantized_pitch(int m);
+teal_status teal_quantize_rows(const void *X, int type, int rows, int m, float t, int8_t *Q, float *row_scale,
+                               void *stream);
+teal_status teal_quantize_rows_swiglu(const float *gate, const float *up, int rows, int m, float t, int8_t *Q,
+                                      float *row_scale, void *stream);
+size_t teal_workspace_bytes_gemm_w8(int rows, int m, int n);
+teal_status teal_gemm_w8(const int8_t *Wq, const void *scale_f16, const int8_t *Q, const float *row_scale, int rows,
+                         float *Y, int m, int n, void *workspace, size_t workspace_bytes, void *stream);
+teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
+                               const int *n, const int8_t *Q, const float *row_scale, int rows, int m,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A mixture of experts for many tokens: the pairs (token, expert) that teal_route_experts chose, sorted by expert, and
+ * the products of every expert with the rows that are its own, however many those are.
+ *
+ * teal_arrange_experts: pair p = token * top_k + slot.
+ *   idx    [tokens][top_k] int32; a number outside [0, experts) is no expert (a padded token).
+ *   order  [tokens * top_k] int32: the pairs of expert 0, those of expert 1 and so on, each expert's in ascending order,
+ *          behind them the pairs without an expert.
+ *   start  [experts + 1] int32: the place in order where each expert's pairs begin, and where the last one's end.
+ *   workspace  at least teal_workspace_bytes_arrange_experts(experts, tokens * top_k) bytes, zero before first use
+ *          like every workspace.
+ *   tokens >= 0, 1 <= top_k <= TEAL_MAX_TOP_K, tokens * top_k <= 2^24, 1 <= experts <= TEAL_MAX_EXPERTS.
+ *
+ * teal_grouped_experts_{bf16,mx4}_gate_up: H[i] = bf16(SiLU(g) * u), g = x W_gate[e]^T, u = x W_up[e]^T, for every place i
+ * of order that has an expert e; x is the row of X of pair order[i]'s token.  Products are exact and summed in fp32;
+ * SiLU(g) * u in the arithmetic stated for teal_sparse_gemv_bf16_swiglu, rounded to bf16.  Rows of H from
+ * start[experts] on are left as they are.
+ *   Wt_gate, Wt_up [experts][m][f] bf16; Wq_* [experts][m][f/2], scale_* [experts] times teal_mx4_scale_bytes(m, f)
+ *          bytes, all 16-byte aligned, as for teal_sparse_experts_*.
+ *   X_bf16 [tokens][m] bf16 (the weights' type: a matrix instruction has one), H_bf16 [tokens * top_k][f] bf16, both
+ *          16-byte aligned.
+ *   m % 8 == 0, f % 8 == 0 (mx4: f % 32 == 0), 8 <= m, f <= 2^20, tokens * top_k as above, and
+ *          (tokens * top_k / 32 + experts) * ceil(f / 128) <= 2^22 (else TEAL_ERR_SHAPE).
+ * teal_grouped_experts_{bf16,mx4}_down:
+ *   y[b] = sum over j of weight[b][j] * (h W_down[e]^T), e = idx[b][j], h = the row of H that belongs to pair (b, j),
+ * j ascending, in fp32.  A pair without an expert adds nothing, whatever its weight.
+ *   Wt_down [experts][m][n] (Wq, scale as above), m = the experts' width, n = the model width.
+ *   idx, order, start: one arrangement; weight [tokens][top_k] fp32; H_bf16 [tokens * top_k][m]; y [tokens][n]
+ *          fp32, fully overwritten.
+ *   workspace  at least teal_workspace_bytes_grouped_experts(tokens * top_k, n) bytes, zero before first use like
+ *          every workspace.
+ * What order and start hold cannot be checked by the host: places and pairs out of range are cut to what there is, so
+ * that nothing outside the arrays is read or written, and the results are then undefined.
+ */
+size_t teal_workspace_bytes_arrange_experts(int experts, int pairs);
+teal_status teal_arrange_experts(const int32_t *idx, int tokens, int top_k, int experts, int32_t *order, int32_t *start,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+teal_status teal_grouped_experts_bf16_gate_up(const void *Wt_gate, const void *Wt_up, int experts, const int32_t *order,
+                                              const int32_t *start, int tokens, int top_k, const void *X_bf16,
+                                              void *H_bf16, int m, int f, void *stream);
+teal_status teal_grouped_experts_mx4_gate_up(const uint8_t *Wq_gate, const uint8_t *scale_gate, const uint8_t *Wq_up,
+                                             const uint8_t *scale_up, int experts, const int32_t *order,
+                                             const int32_t *start, int tokens, int top_k, const void *X_bf16,
+                                             void *H_bf16, int m, int f, void *stream);
+size_t teal_workspace_bytes_grouped_experts(int pairs, int n);
+teal_status teal_grouped_experts_bf16_down(const void *Wt_down, int experts, const int32_t *order, const int32_t *start,
+                                           int tokens, int top_k, const int32_t *idx, const float *weight,
+                                           const void *H_bf16, float *y, int m, int n, void *workspace,
+                                           size_t workspace_bytes, void *stream);
+teal_status teal_grouped_experts_mx4_down(const uint8_t *Wq_down, const uint8_t *scale_down, int experts,
+                                          const int32_t *order, const int32_t *start, int tokens, int top_k,
+                                          const int32_t *idx, const float *weight, const void *H_bf16, float *y,
+                                          int m, int n, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * The MLP of a Transformer block in ONE kernel launch (Appendix A.3):
  *     MLP(x) = (SiLU(x W_gate^T) . x W_up^T) W_down^T,
  * with every product thresholded (Section 4.2): gate = s_{t_gate}(x) W_gate^T,

@@ -31,4 +31,9 @@ from .binding import (  # noqa: F401
     TEAL_MAX_EXPERTS, TEAL_MAX_TOP_K, TEAL_SCORE_SOFTMAX, TEAL_SCORE_SIGMOID, teal_route_experts,
     teal_workspace_bytes_experts, teal_sparse_experts_bf16, teal_sparse_experts_mx4,
     teal_sparse_experts_bf16_swiglu, teal_sparse_experts_mx4_swiglu,
+    TEAL_F16, TEAL_BF16, TEAL_MAX_ROWS, TEAL_MAX_ROW_SUM,
+    teal_quantized_pitch, teal_quantize_rows, teal_quantize_rows_swiglu, teal_workspace_bytes_gemm_w8,
+    teal_gemm_w8, teal_gemm_w8_multi, teal_workspace_bytes_arrange_experts, teal_arrange_experts,
+    teal_grouped_experts_bf16_gate_up, teal_grouped_experts_mx4_gate_up, teal_workspace_bytes_grouped_experts,
+    teal_grouped_experts_bf16_down, teal_grouped_experts_mx4_down,
 )

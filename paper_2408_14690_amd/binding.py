@@ -48,6 +48,10 @@ EXPORTS = (
     "teal_sparse_gemv_mx4_multi", "teal_sparse_gemv_mx4_swiglu", "teal_sparse_gemv_mx4_rmsnorm_multi",
     "teal_route_experts", "teal_workspace_bytes_experts", "teal_sparse_experts_bf16",
     "teal_sparse_experts_mx4", "teal_sparse_experts_bf16_swiglu", "teal_sparse_experts_mx4_swiglu",
+    "teal_quantized_pitch", "teal_quantize_rows", "teal_quantize_rows_swiglu", "teal_workspace_bytes_gemm_w8",
+    "teal_gemm_w8", "teal_gemm_w8_multi", "teal_workspace_bytes_arrange_experts", "teal_arrange_experts",
+    "teal_grouped_experts_bf16_gate_up", "teal_grouped_experts_mx4_gate_up", "teal_workspace_bytes_grouped_experts",
+    "teal_grouped_experts_bf16_down", "teal_grouped_experts_mx4_down",
 )
 TEAL_HIST_BINS = 32768
 TEAL_MAX_BATCH = 8
@@ -55,6 +59,10 @@ TEAL_MAX_EXPERTS = 1024
 TEAL_MAX_TOP_K = 32
 TEAL_SCORE_SOFTMAX = 0
 TEAL_SCORE_SIGMOID = 1
+TEAL_F16 = 0
+TEAL_BF16 = 1
+TEAL_MAX_ROWS = 1048576
+TEAL_MAX_ROW_SUM = 131072
 
 
 class MlpShape(ctypes.Structure):
@@ -235,6 +243,32 @@ def load_library():
     lib.teal_sparse_experts_bf16_swiglu.argtypes = [vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp, sz, vp]
     lib.teal_sparse_experts_mx4_swiglu.restype = i
     lib.teal_sparse_experts_mx4_swiglu.argtypes = [vp, vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp, sz, vp]
+    lib.teal_quantized_pitch.restype = i
+    lib.teal_quantized_pitch.argtypes = [i]
+    lib.teal_quantize_rows.restype = i
+    lib.teal_quantize_rows.argtypes = [vp, i, i, i, f, vp, vp, vp]
+    lib.teal_quantize_rows_swiglu.restype = i
+    lib.teal_quantize_rows_swiglu.argtypes = [vp, vp, i, i, f, vp, vp, vp]
+    lib.teal_workspace_bytes_gemm_w8.restype = sz
+    lib.teal_workspace_bytes_gemm_w8.argtypes = [i, i, i]
+    lib.teal_gemm_w8.restype = i
+    lib.teal_gemm_w8.argtypes = [vp, vp, vp, vp, i, vp, i, i, vp, sz, vp]
+    lib.teal_gemm_w8_multi.restype = i
+    lib.teal_gemm_w8_multi.argtypes = [i, vp, vp, vp, vp, vp, vp, i, i, vp, sz, vp]
+    lib.teal_workspace_bytes_arrange_experts.restype = sz
+    lib.teal_workspace_bytes_arrange_experts.argtypes = [i, i]
+    lib.teal_arrange_experts.restype = i
+    lib.teal_arrange_experts.argtypes = [vp, i, i, i, vp, vp, vp, sz, vp]
+    lib.teal_grouped_experts_bf16_gate_up.restype = i
+    lib.teal_grouped_experts_bf16_gate_up.argtypes = [vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp]
+    lib.teal_grouped_experts_mx4_gate_up.restype = i
+    lib.teal_grouped_experts_mx4_gate_up.argtypes = [vp, vp, vp, vp, i, vp, vp, i, i, vp, vp, i, i, vp]
+    lib.teal_workspace_bytes_grouped_experts.restype = sz
+    lib.teal_workspace_bytes_grouped_experts.argtypes = [i, i]
+    lib.teal_grouped_experts_bf16_down.restype = i
+    lib.teal_grouped_experts_bf16_down.argtypes = [vp, i, vp, vp, i, i, vp, vp, vp, vp, i, i, vp, sz, vp]
+    lib.teal_grouped_experts_mx4_down.restype = i
+    lib.teal_grouped_experts_mx4_down.argtypes = [vp, vp, i, vp, vp, i, i, vp, vp, vp, vp, i, i, vp, sz, vp]
     ip = c.POINTER(c.c_int)
     lib.teal_gemv_plan.restype = i
     lib.teal_gemv_plan.argtypes = [i, i, i, ip, ip, ip, ip, ip]
@@ -1069,4 +1103,142 @@ def teal_sparse_experts_mx4_swiglu(Wq, scale, t, y, experts, idx, weight, tokens
         _expert_floats(t, experts, "t"), _ptr(y, 4 * tokens * n, "y"), int(experts), _expert_numbers(idx, pairs),
         _expert_floats(weight, pairs, "weight"), int(tokens), int(top_k), _ptr(gate, 4 * pairs * m, "gate"),
         _ptr(up, 4 * pairs * m, "up"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+        _stream(stream))
+
+
+def teal_quantized_pitch(m: int) -> int:
+    return int(load_library().teal_quantized_pitch(int(m)))
+
+
+def _pitch_need(m):
+    """Bytes of a row of 8-bit integers; what a call with another m is refused for is left to it."""
+    return (m + 127) // 128 * 128
+
+
+def _of_bytes(a, size, what, kind):
+    """Refuses a tensor whose values have another size than the call takes them to have."""
+    if getattr(a, "element_size", None) is not None and a.element_size() != size:
+        raise ValueError(f"{what}: {kind}")
+    return a
+
+
+def _row_floats(a, count, what):
+    return _ptr(_of_bytes(a, 4, what, "32-bit floats"), 4 * count, what)
+
+
+def teal_quantize_rows(X, type, rows, m, t, Q, row_scale, stream=None) -> int:
+    """type: TEAL_F16 or TEAL_BF16; a torch tensor has to be of it."""
+    dtype = str(getattr(X, "dtype", ""))
+    if dtype.startswith("torch.") and dtype in ("torch.float16", "torch.bfloat16") and \
+            (dtype == "torch.bfloat16") != (int(type) == TEAL_BF16):
+        raise ValueError(f"X: a tensor of {dtype}, and type says another")
+    return _call(
+        "teal_quantize_rows",
+        _ptr(_of_bytes(X, 2, "X", "16-bit floats"), 2 * rows * m, "X"), int(type), int(rows), int(m), float(t),
+        _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
+
+
+def teal_quantize_rows_swiglu(gate, up, rows, m, t, Q, row_scale, stream=None) -> int:
+    return _call(
+        "teal_quantize_rows_swiglu",
+        _row_floats(gate, rows * m, "gate"), _row_floats(up, rows * m, "up"), int(rows), int(m), float(t),
+        _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
+
+
+def teal_workspace_bytes_gemm_w8(rows: int, m: int, n: int) -> int:
+    return int(load_library().teal_workspace_bytes_gemm_w8(int(rows), int(m), int(n)))
+
+
+def teal_gemm_w8(Wq, scale_f16, Q, row_scale, rows, Y, m, n, workspace, workspace_bytes=None, stream=None) -> int:
+    return _call(
+        "teal_gemm_w8",
+        _ptr(Wq, m * n, "Wq"), _ptr(scale_f16, 2 * n, "scale"), _ptr(Q, rows * _pitch_need(m), "Q"),
+        _row_floats(row_scale, rows, "row_scale"), int(rows), _row_floats(Y, rows * n, "Y"), int(m), int(n),
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_gemm_w8_multi(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m, workspace, workspace_bytes=None,
+                       stream=None) -> int:
+    """len(Wq_list) matrices on the same rows; the per-matrix lists become host arrays."""
+    count = len(Wq_list)
+    if not (len(scale_list) == len(Y_list) == len(n_list) == count):
+        raise ValueError("per-matrix lists must have the same length")
+    W = _pointers([_ptr(w, m * n, "Wq") or 0 for w, n in zip(Wq_list, n_list)])
+    S = _pointers([_ptr(sc, 2 * n, "scale") or 0 for sc, n in zip(scale_list, n_list)])
+    Y = _pointers([_row_floats(y, rows * n, "Y") or 0 for y, n in zip(Y_list, n_list)])
+    return _call(
+        "teal_gemm_w8_multi",
+        count, W, S, Y, _ints(n_list), _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"),
+        int(rows), int(m), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_workspace_bytes_arrange_experts(experts: int, pairs: int) -> int:
+    return int(load_library().teal_workspace_bytes_arrange_experts(int(experts), int(pairs)))
+
+
+def _numbers(a, count, what):
+    return _ptr(_of_bytes(a, 4, what, "32-bit integers"), 4 * count, what)
+
+
+def teal_arrange_experts(idx, tokens, top_k, experts, order, start, workspace, workspace_bytes=None, stream=None) -> int:
+    pairs = tokens * top_k
+    return _call(
+        "teal_arrange_experts",
+        _expert_numbers(idx, pairs), int(tokens), int(top_k), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def _bf16_rows(a, count, what):
+    dtype = str(getattr(a, "dtype", ""))
+    if dtype == "torch.float16":
+        raise ValueError(f"{what}: bf16 numbers")
+    return _ptr(_of_bytes(a, 2, what, "bf16 numbers"), 2 * count, what)
+
+
+def teal_grouped_experts_bf16_gate_up(Wt_gate, Wt_up, experts, order, start, tokens, top_k, X_bf16, H_bf16, m, f,
+                                      stream=None) -> int:
+    """H: a row per place of `order`, of the experts' width f."""
+    pairs, need = tokens * top_k, 2 * experts * m * f
+    return _call(
+        "teal_grouped_experts_bf16_gate_up",
+        _ptr(Wt_gate, need, "Wt_gate"), _ptr(Wt_up, need, "Wt_up"), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16_rows(X_bf16, tokens * m, "X"),
+        _bf16_rows(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
+
+
+def teal_grouped_experts_mx4_gate_up(Wq_gate, scale_gate, Wq_up, scale_up, experts, order, start, tokens, top_k, X_bf16,
+                                     H_bf16, m, f, stream=None) -> int:
+    pairs, codes, scales = tokens * top_k, experts * (m * f // 2), experts * _mx4_scale_need(m, f)
+    return _call(
+        "teal_grouped_experts_mx4_gate_up",
+        _ptr(Wq_gate, codes, "Wq_gate"), _ptr(scale_gate, scales, "scale_gate"), _ptr(Wq_up, codes, "Wq_up"),
+        _ptr(scale_up, scales, "scale_up"), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16_rows(X_bf16, tokens * m, "X"),
+        _bf16_rows(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
+
+
+def teal_workspace_bytes_grouped_experts(pairs: int, n: int) -> int:
+    return int(load_library().teal_workspace_bytes_grouped_experts(int(pairs), int(n)))
+
+
+def teal_grouped_experts_bf16_down(Wt_down, experts, order, start, tokens, top_k, idx, weight, H_bf16, y, m, n,
+                                   workspace, workspace_bytes=None, stream=None) -> int:
+    pairs = tokens * top_k
+    return _call(
+        "teal_grouped_experts_bf16_down",
+        _ptr(Wt_down, 2 * experts * m * n, "Wt_down"), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _expert_numbers(idx, pairs),
+        _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"), _row_floats(y, tokens * n, "y"),
+        int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_grouped_experts_mx4_down(Wq_down, scale_down, experts, order, start, tokens, top_k, idx, weight, H_bf16, y, m,
+                                  n, workspace, workspace_bytes=None, stream=None) -> int:
+    pairs = tokens * top_k
+    return _call(
+        "teal_grouped_experts_mx4_down",
+        _ptr(Wq_down, experts * (m * n // 2), "Wq_down"), _ptr(scale_down, experts * _mx4_scale_need(m, n), "scale_down"),
+        int(experts), _numbers(order, pairs, "order"), _numbers(start, experts + 1, "start"), int(tokens), int(top_k),
+        _expert_numbers(idx, pairs), _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"),
+        _row_floats(y, tokens * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream))

@@ -18,7 +18,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libteal.so")
 
 SOURCES = ("teal_api.cpp", "sparsify_pack.hip", "gemv_bf16.hip", "gemv_wq.hip", "gemv_batch.hip",
-           "gemv_mx4.hip", "route_experts.hip", "calibrate.hip")
+           "gemv_mx4.hip", "route_experts.hip", "calibrate.hip", "gemm_w8.hip", "grouped_experts.hip")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,348 @@
+// Products of many rows on the matrix cores: a thread block's tile of Y = X W, X rows contiguous along the sum, W
+// input-channel-major as the one-row products store it (Wt[m][n], n contiguous).
+//
+// A block takes BM rows by BN columns and walks the sum in slabs of 128 bytes of a row of X: 64 channels of bf16, 128 of
+// int8.  X and W travel from memory into LDS without registers (global_load_lds), in a ring of STAGES slabs: one
+// barrier a slab, the loads of the slab STAGES - 1 further in flight while a slab is multiplied.  The matrix
+// instructions (16 x 16, K = 32 for bf16, 64 for int8) want both operands contiguous along the sum in a lane; X is, and W comes
+// through the transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block of 16-bit values and get a
+// column each; ds_read_b64_tr_b8: an 8 x 16 block of bytes).  W is the first operand and X the second, so a lane ends
+// up with four neighbouring columns of one row, 16 bytes of y.
+//
+// LDS banks.  A row of X in LDS is 128 bytes, 8 chunks of 16: chunk c of row r is at place c ^ (r & 7), so 8 lanes
+// that read one chunk of 8 rows touch all banks.  A row of W has 32-byte units (bf16) or 16-byte units (int8), what one
+// row gives to a transposing read: unit u of channel k is at place u ^ swizzle(k), so that the 4 (8) rows of a group of
+// 16 lanes, and the groups of two halves of a wavefront, touch different banks.  The direct loads fill LDS linearly; the
+// permutation is in the lanes' global addresses, within one row's bytes.
+#pragma once
+
+#include "gemv_common.h"
+
+namespace teal {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kSlabBytes = 128;            // of a row of X
+
+// Source of the zeros for channels past the last one.
+static __device__ const u32x4 zero_chunk = {0u, 0u, 0u, 0u};
+
+// 16 bytes per lane from `from` to LDS at `to` (wavefront-uniform) + 16 * lane.  The wait is the caller's.  In assembly,
+// because the compiler, which cannot know which part of LDS a load fills, waits for all of them before any LDS read
+// that follows.  m0 is written right before it is read, and nothing else in these kernels uses it.
+__device__ __forceinline__ void load_to_lds(const unsigned char *from, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to));
+}
+// Waits until at most `left` of this wavefront's vector-memory operations are under way and all its LDS operations are
+// done, then for the block.  Afterwards what every wavefront loaded before is in LDS, and nobody reads what it read.
+template <int left>
+__device__ __forceinline__ void wait_and_meet()
+{
+    static_assert(left >= 0 && left < 64, "six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory");
+}
+
+__device__ __forceinline__ unsigned lds_address(const void *p)
+{
+    typedef const __attribute__((address_space(3))) unsigned char *lds_ptr;
+    return (unsigned)(uintptr_t)(lds_ptr)p;
+}
+
+// How W is stored.
+struct WeightsBf16 {
+    static constexpr int kBytes = 2;               // of a value in LDS
+    static constexpr int kSlabRows = 64;           // channels of a slab
+    static constexpr bool kMx4 = false;
+    typedef f32x4 Acc;
+};
+struct WeightsInt8 {
+    static constexpr int kBytes = 1;
+    static constexpr int kSlabRows = 128;
+    static constexpr bool kMx4 = false;
+    typedef i32x4 Acc;
+};
+// Microscaled 4-bit numbers, made bf16 numbers (exactly, by the hardware's conversion with a scale) on their way: codes
+// and scales come into the ring, every thread converts one block of 32 a slab, one slab ahead of its use, and a second
+// pair of buffers has the bf16 tile.
+struct WeightsMx4 {
+    static constexpr int kBytes = 2;
+    static constexpr int kSlabRows = 64;
+    static constexpr bool kMx4 = true;
+    typedef f32x4 Acc;
+};
+
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+struct TileShape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;       // 16 x 16 pieces of a wavefront
+};
+
+// The product of one tile.  HALVES = 1: the tile's BN columns are neighbours in one matrix; 2: BN / 2 columns of each of
+// two matrices, and piece f of a wavefront and piece f + NF / 2 are the same columns of the two.
+template <class F, class S, int HALVES>
+struct TileProduct {
+    static constexpr int BM = S::BM, BN = S::BN, MF = S::MF, NF = S::NF, STAGES = S::STAGES;
+    static constexpr int kRowBytes = BN * F::kBytes;                   // of W in LDS
+    static constexpr int kSlabX = BM * kSlabBytes, kSlabW = F::kSlabRows * kRowBytes;
+    static constexpr int kCodes = F::kSlabRows * BN / 2, kScales = HALVES * F::kSlabRows * 16;     // of mx4, in a slab
+    static constexpr int kStage = kSlabX + (F::kMx4 ? kCodes + kScales : kSlabW);
+    static constexpr int kRing = STAGES * kStage;
+    static constexpr int kLds = kRing + (F::kMx4 ? 2 * kSlabW : 0);
+    static constexpr int kLoadsX = (BM / 8 + S::kWaves - 1) / S::kWaves;       // of 64 lanes x 16 bytes, a wavefront's
+    static constexpr int kLoadsW = F::kMx4 ? 2 : kSlabW / 1024 / S::kWaves;    // mx4: codes and scales
+    static constexpr int kRowsPerLoad = 1024 / kRowBytes;              // rows of W that a wavefront's load covers
+    static constexpr int kRowStep = kRowsPerLoad * S::kWaves;
+    static constexpr int kUnit = F::kBytes == 2 ? 32 : 16;             // bytes that a permutation keeps together
+    static constexpr int kUnitMask = kRowBytes / HALVES / kUnit < 16 ? kRowBytes / HALVES / kUnit - 1 : 15;
+    static constexpr int kHalfCols = BN / HALVES;
+    static_assert(BM % (16 * S::WM) == 0 && BN % (16 * S::WN) == 0 && kSlabW % (1024 * S::kWaves) == 0, "");
+    static_assert(!F::kMx4 || (kCodes == 16 * S::kThreads && S::kWaves >= HALVES), "a block of 32 codes per thread");
+    static_assert(HALVES == 1 || NF % 2 == 0, "both matrices in every wavefront");
+    static_assert(kRowStep % 32 == 0 || (F::kBytes == 2 && kRowStep % 16 == 0), "a lane's permutation is the same in all its loads");
+    static_assert(kLds <= 160 * 1024, "");
+
+    typedef typename F::Acc Acc;
+    Acc acc[MF][NF];
+
+    static __device__ __forceinline__ int swizzle(int k)
+    {
+        return (F::kBytes == 2 ? (k & 3) | (k >> 3 & 1) << 2 : (k & 7) | (k >> 4 & 1) << 3) & kUnitMask;
+    }
+
+    unsigned lds;                                // of the ring
+    int wave, lane, wm, wn;
+    const unsigned char *x_lane[kLoadsX];        // this lane's chunk of its rows, first channel
+    const unsigned char *w_lane;                 // this lane's columns, its row of the first load, first channel of the sum
+    long long w_pitch;                           // bytes
+    int x_chunk, w_row;                          // chunk of the row and row of the slab that the lane loads
+    // mx4: this lane's 16 bytes of scales, which come in tiles of 8 channels by 16 blocks; where the scale and the numbers
+    // of its codes are
+    const unsigned char *s_lane;
+    int s_pitch;                                 // bytes between tiles of one block row
+    unsigned scale_at, value_at[4];
+
+    // `row_of(r)`: the address of the tile's row r of X (of any valid row where the tile has none).  `w_of(half)`: of the
+    // matrix; `scale_of(half)`: of its scales (mx4).  Columns from n on repeat the last ones (n a multiple of a chunk): they
+    // are not stored.
+    template <class RowOf, class WOf, class ScaleOf>
+    __device__ __forceinline__ void begin(void *smem, const RowOf &row_of, const WOf &w_of, const ScaleOf &scale_of,
+                                          int col0, int n)
+    {
+        lds = lds_address(smem);
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = wave / S::WN;
+        wn = wave % S::WN;
+        x_chunk = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+        for (int j = 0; j < kLoadsX; ++j)
+            x_lane[j] = row_of(x_load(j) * 8 + (lane >> 3)) + 16 * x_chunk;
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) acc[i][f] = Acc{};
+        const int at = (wave * 64 + lane) * 16;                        // in a slab
+        if constexpr (F::kMx4) {
+            constexpr int kBlocks = BN / 32 / HALVES;                  // of a row of one matrix
+            w_row = threadIdx.x / (BN / 32);
+            const int half = threadIdx.x % (BN / 32) / kBlocks, in_half = threadIdx.x % kBlocks;
+            const int col = min(col0 + 32 * in_half, n - 32);
+            w_pitch = n / 2;
+            w_lane = w_of(half) + w_row * w_pitch + col / 2;
+            // a wavefront loads the slab's scales of one matrix: lane / 8 the tile, lane % 8 the channel in it
+            s_pitch = mx4_scale_tiles(n) * kMx4TileBytes;
+            s_lane = scale_of(wave % HALVES) + (long long)(lane >> 3) * s_pitch + col0 / 512 * kMx4TileBytes + (lane & 7) * 16;
+            scale_at = kSlabX + kCodes + half * (kScales / HALVES) + (w_row / 8) * kMx4TileBytes + w_row % 8 * 16 + col / 32 % 16;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                value_at[q] = w_row * kRowBytes + half * (kRowBytes / HALVES) +
+                              ((2 * in_half + q / 2) ^ swizzle(w_row)) * 32 + q % 2 * 16;
+            return;
+        }
+        w_row = at / kRowBytes;
+        const int half = HALVES == 1 ? 0 : at % kRowBytes / (kRowBytes / 2);
+        const int in_half = at % (kRowBytes / HALVES);
+        const int unit = in_half / kUnit ^ swizzle(w_row);
+        const int col = min(col0 + (unit * kUnit + in_half % kUnit) / F::kBytes, n - 16 / F::kBytes);
+        w_pitch = (long long)n * F::kBytes;
+        w_lane = w_of(half) + w_row * w_pitch + (long long)col * F::kBytes;
+    }
+    // Which 8 rows of X the wavefront's load j takes: where there are fewer loads than wavefronts some load the same.
+    __device__ __forceinline__ int x_load(int j) const { return (wave + j * S::kWaves) % (BM / 8); }
+
+    // Slab `slab` of a sum of m channels into place `stage` of the ring: X, and W.  Channels from m on are zeros.
+    __device__ __forceinline__ void load_x(int slab, int stage, int m)
+    {
+        const unsigned to = lds + stage * kStage;
+        const long long x_at = (long long)slab * kSlabBytes;
+        const int k0 = slab * F::kSlabRows;
+        const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
+        // (rows of 8-bit integers have zeros behind their end)
+        if (F::kBytes == 1 || k0 + F::kSlabRows <= m) {
+#pragma unroll
+            for (int j = 0; j < kLoadsX; ++j) load_to_lds(x_lane[j] + x_at, to + x_load(j) * 1024);
+        } else {
+            const bool in_row = k0 + x_chunk * (16 / F::kBytes) < m;
+#pragma unroll
+            for (int j = 0; j < kLoadsX; ++j) load_to_lds(in_row ? x_lane[j] + x_at : zero, to + x_load(j) * 1024);
+        }
+    }
+    __device__ __forceinline__ void load_w(int slab, int stage, int m)
+    {
+        const unsigned to = lds + stage * kStage + kSlabX + wave * 1024;
+        const int k0 = slab * F::kSlabRows;
+        const unsigned char *const w_at = w_lane + k0 * w_pitch;
+        const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
+        if constexpr (F::kMx4) {
+            load_to_lds(k0 + w_row < m ? w_at : zero, to);
+            const unsigned char *const s_at = s_lane + (long long)(k0 / 8) * s_pitch;
+            load_to_lds(k0 + (lane & ~7) < m ? s_at : zero, lds + stage * kStage + kSlabX + kCodes + wave % HALVES * 1024);
+        } else if (k0 + F::kSlabRows <= m) {
+#pragma unroll
+            for (int j = 0; j < kLoadsW; ++j) load_to_lds(w_at + j * kRowStep * w_pitch, to + j * S::kWaves * 1024);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kLoadsW; ++j)
+                load_to_lds(k0 + w_row + j * kRowStep < m ? w_at + j * kRowStep * w_pitch : zero,
+                            to + j * S::kWaves * 1024);
+        }
+    }
+
+    // mx4: the codes of slab `slab` at `stage` of the ring to bf16 numbers in buffer `to`.
+    __device__ __forceinline__ void convert(int slab, int stage, int to, int m)
+    {
+        typedef const __attribute__((address_space(3))) unsigned char *lds_ptr;
+        typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+        typedef __attribute__((address_space(3))) u32x4 *lds_out;
+        const lds_ptr from = (lds_ptr)(uintptr_t)(lds + stage * kStage);
+        const u32x4 codes = *(lds_u32x4)(from + kSlabX + threadIdx.x * 16);
+        // what lies behind the last channel of a tile of scales has no meaning
+        const unsigned byte = slab * F::kSlabRows + w_row < m ? from[scale_at] : 0u;
+        const float sc = __uint_as_float(byte << 23);
+        const unsigned buffer = lds + kRing + to * kSlabW;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            u32x4 v;
+            v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 0));
+            v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 1));
+            v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 2));
+            v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 3));
+            *(lds_out)(uintptr_t)(buffer + value_at[q]) = v;
+        }
+    }
+
+    // Multiplies in a slab whose X is at `x_at` and whose W is at `w_at` in LDS.
+    __device__ __forceinline__ void multiply(unsigned x_at, unsigned w_at)
+    {
+        typedef const __attribute__((address_space(3))) unsigned char *lds_ptr;
+        typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+        const lds_ptr x = (lds_ptr)(uintptr_t)x_at, w = (lds_ptr)(uintptr_t)w_at;
+        const int l = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            u32x4 W[NF];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const int half = HALVES == 1 ? 0 : f / (NF / 2);
+                const int piece = HALVES == 1 ? wn * NF + f : wn * (NF / 2) + f % (NF / 2);
+                if constexpr (F::kBytes == 2) {
+                    typedef short s16x4 __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+                    const int k = 32 * ks + 8 * g + l / 4;             // and 4 further
+                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 + l % 4 * 8;
+                    const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
+                    const uint2 b = __builtin_bit_cast(
+                        uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * kRowBytes)));
+                    W[f] = u32x4{a.x, a.y, b.x, b.y};
+                } else {
+                    typedef int i32x2 __attribute__((ext_vector_type(2)));
+                    typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
+                    const int k = 64 * ks + 16 * g + l / 2;            // and 8 further
+                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 16 + l % 2 * 8;
+                    const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)p));
+                    const uint2 b = __builtin_bit_cast(
+                        uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(p + 8 * kRowBytes)));
+                    W[f] = u32x4{a.x, a.y, b.x, b.y};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                const int row = (wm * MF + i) * 16 + l;
+                const u32x4 X = *(lds_u32x4)(x + row * kSlabBytes + ((4 * ks + g) ^ (l & 7)) * 16);
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    if constexpr (F::kBytes == 2)
+                        acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, W[f]), __builtin_bit_cast(bf16x8, X), acc[i][f], 0, 0, 0);
+                    else
+                        acc[i][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                            __builtin_bit_cast(i32x4, W[f]), __builtin_bit_cast(i32x4, X), acc[i][f], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // Slabs [first, last) of a sum of m channels.
+    __device__ __forceinline__ void run(int first, int last, int m)
+    {
+        constexpr int kLoads = kLoadsX + kLoadsW;
+        constexpr int kAhead = F::kMx4 ? 1 : 0;          // by how many slabs W is ahead of X
+        if constexpr (F::kMx4) {
+            load_w(first, STAGES - 1, m);
+            wait_and_meet<0>();
+            convert(first, STAGES - 1, 0, m);      // (the place is filled again after the next meeting)
+        }
+        // Place s of the ring: X of slab first + s, and W of the same slab (mx4: of the next one).
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) {
+            if (first + s < last) load_x(first + s, s, m);
+            if (first + s + kAhead < last) load_w(first + s + kAhead, s, m);
+        }
+        int stage = 0, buffer = 0;
+        for (int slab = first; slab < last; ++slab) {
+            // what later slabs loaded may still be under way
+            if (slab + STAGES - 2 + kAhead < last)
+                wait_and_meet<(STAGES - 2) * kLoads>();
+            else
+                wait_and_meet<0>();
+            const int next = slab + STAGES - 1, to = stage == 0 ? STAGES - 1 : stage - 1;
+            if (next < last) load_x(next, to, m);
+            if (next + kAhead < last) load_w(next + kAhead, to, m);
+            const unsigned x_at = lds + stage * kStage;
+            multiply(x_at, F::kMx4 ? lds + kRing + buffer * kSlabW : x_at + kSlabX);
+            if constexpr (F::kMx4) {
+                if (slab + 1 < last) convert(slab + 1, stage, buffer ^ 1, m);
+                buffer ^= 1;
+            }
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+        }
+    }
+
+    // Row of the tile and first of four neighbouring columns (of a half) that acc[i][f] holds.
+    __device__ __forceinline__ int row_of(int i) const { return (wm * MF + i) * 16 + (lane & 15); }
+    __device__ __forceinline__ int col_of(int f) const
+    {
+        const int piece = HALVES == 1 ? wn * NF + f : wn * (NF / 2) + f % (NF / 2);
+        return piece * 16 + 4 * (lane >> 4);
+    }
+};
+
+// Order of the tiles: neighbours in it share an XCD (its blocks are every eighth of the grid), and the blocks that run there
+// together are 8 row tiles by as many column tiles, so that what they read of X and of W is read once into its L2.
+constexpr int kXcds = 8;
+constexpr int kRowTileGroup = 8;
+// Place `at` among row_tiles x col_tiles of them: row tile and column tile.
+__device__ __forceinline__ int2 tile_at(int at, int row_tiles, int col_tiles)
+{
+    const int group = at / (kRowTileGroup * col_tiles), in_group = at - group * kRowTileGroup * col_tiles;
+    const int rows = min(kRowTileGroup, row_tiles - group * kRowTileGroup);
+    return make_int2(group * kRowTileGroup + in_group % rows, in_group / rows);
+}
+
+}  // namespace teal

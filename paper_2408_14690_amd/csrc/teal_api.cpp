@@ -1473,6 +1473,254 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
     return experts_call(4, h, workspace, workspace_bytes, stream);
 }
 
+// ---- many rows ----
+
+static_assert(TEAL_MAX_ROW_SUM == teal::kMaxRowSum, "the limit the header states is the kernel's");
+
+// A launch holds fewer than 2^32 threads: tiles of 32 rows by 128 columns, the smallest, have 256 each.
+static constexpr long long kMaxTiles = 1 << 22;
+
+int teal_quantized_pitch(int m) { return m < 1 || m > TEAL_MAX_ROW_SUM ? 0 : teal::quantized_pitch(m); }
+
+static teal_status check_quantize(int rows, int m, float t, const void *Q, const void *row_scale, const void *x,
+                                  const void *x2, int align)
+{
+    if (rows < 0 || rows > TEAL_MAX_ROWS || m < 1 || m > TEAL_MAX_ROW_SUM) return TEAL_ERR_SHAPE;
+    if (rows > 0 && (!Q || !row_scale || !x || !x2)) return TEAL_ERR_NULL;
+    if (!aligned(Q, 16) || !aligned(row_scale, 4) || !aligned(x, align) || !aligned(x2, align)) return TEAL_ERR_ALIGN;
+    if (!threshold_ok(t)) return TEAL_ERR_THRESHOLD;
+    return TEAL_OK;
+}
+
+teal_status teal_quantize_rows(const void *X, int type, int rows, int m, float t, int8_t *Q, float *row_scale,
+                               void *stream)
+{
+    const teal_status st = check_quantize(rows, m, t, Q, row_scale, X, X, 2);
+    if (st != TEAL_OK) return st;
+    if (type != TEAL_F16 && type != TEAL_BF16) return TEAL_ERR_UNSUPPORTED;
+    if (rows == 0) return TEAL_OK;
+    return from_hip(teal::launch_quantize_rows(X, type == TEAL_BF16, rows, m, t, Q, row_scale,
+                                               static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_quantize_rows_swiglu(const float *gate, const float *up, int rows, int m, float t, int8_t *Q,
+                                      float *row_scale, void *stream)
+{
+    const teal_status st = check_quantize(rows, m, t, Q, row_scale, gate, up, 4);
+    if (st != TEAL_OK) return st;
+    if (rows == 0) return TEAL_OK;
+    return from_hip(teal::launch_quantize_rows_swiglu(gate, up, rows, m, t, Q, row_scale,
+                                                      static_cast<hipStream_t>(stream)));
+}
+
+// Shape of the products of `rows` rows with matrices of widths n.
+static teal::GemmShape gemm_w8_shape(int rows, int m, const int *n, int count)
+{
+    auto col_tiles = [&](int bn) {
+        long long tiles = 0;
+        for (int k = 0; k < count; ++k) tiles += (n[k] + bn - 1) / bn;
+        return tiles;
+    };
+    teal::GemmShape s{256, 256, 1};
+    if (rows <= 64) s = {32, 128, 1};
+    else if (rows <= 512 || (long long)((rows + 255) / 256) * col_tiles(256) < 192) s = {128, 128, 1};
+    const long long tiles = (long long)((rows + s.bm - 1) / s.bm) * col_tiles(s.bn);
+    const int slabs = teal::quantized_pitch(m) / 128;
+    if (s.bm < 256)
+        while (tiles * s.splits * 2 <= 512 && slabs >= s.splits * 2) s.splits *= 2;
+    return s;
+}
+
+// Sums of the slices: of at most 512 blocks.
+static constexpr size_t kGemmPartialBytes = 512 * (size_t)(128 * 128 * 4);
+
+size_t teal_workspace_bytes_gemm_w8(int rows, int m, int n)
+{
+    if (rows < 0 || rows > TEAL_MAX_ROWS || m < 1 || m > TEAL_MAX_ROW_SUM || n < 16 || n > teal::kMaxDim) return 0;
+    return teal::kCounterBytes + kGemmPartialBytes;
+}
+
+teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
+                               const int *n, const int8_t *Q, const float *row_scale, int rows, int m, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    if (count < 1 || count > teal::kMaxMatrices) return TEAL_ERR_UNSUPPORTED;
+    if (!Wq || !scale_f16 || !Y || !n || !workspace) return TEAL_ERR_NULL;
+    if (rows < 0 || rows > TEAL_MAX_ROWS || m < 1 || m > TEAL_MAX_ROW_SUM) return TEAL_ERR_SHAPE;
+    if (rows > 0 && (!Q || !row_scale)) return TEAL_ERR_NULL;
+    long long n_total = 0, col_tiles = 0;
+    for (int k = 0; k < count; ++k) {
+        if (!Wq[k] || !scale_f16[k] || (rows > 0 && !Y[k])) return TEAL_ERR_NULL;
+        if (n[k] < 16 || n[k] > teal::kMaxDim || n[k] % 16 != 0) return TEAL_ERR_SHAPE;
+        n_total += n[k];
+        col_tiles += (n[k] + 127) / 128;
+    }
+    if (n_total > teal::kMaxDim || (long long)((rows + 31) / 32) * col_tiles > kMaxTiles) return TEAL_ERR_SHAPE;
+    for (int k = 0; k < count; ++k)
+        if (!aligned(Wq[k], 16) || !aligned(scale_f16[k], 2) || !aligned(Y[k], 4)) return TEAL_ERR_ALIGN;
+    if (!aligned(Q, 16) || !aligned(row_scale, 4) || !aligned(workspace, kAlignWorkspace)) return TEAL_ERR_ALIGN;
+    if (workspace_bytes < teal_workspace_bytes_gemm_w8(rows, m, (int)n_total)) return TEAL_ERR_WORKSPACE;
+    if (rows == 0) return TEAL_OK;
+    const teal::GemmW8HostArgs h{count, Wq, scale_f16, Y, n, Q, row_scale, rows, m, ws_counters(workspace),
+                                 ws_counters(workspace) + teal::kCounterBytes / sizeof(int)};
+    return from_hip(teal::launch_gemm_w8(h, gemm_w8_shape(rows, m, n, count), static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_gemm_w8(const int8_t *Wq, const void *scale_f16, const int8_t *Q, const float *row_scale, int rows,
+                         float *Y, int m, int n, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return teal_gemm_w8_multi(1, &Wq, &scale_f16, &Y, &n, Q, row_scale, rows, m, workspace, workspace_bytes, stream);
+}
+
+static bool pairs_ok(int tokens, int top_k)
+{
+    return tokens >= 0 && top_k >= 1 && top_k <= TEAL_MAX_TOP_K && (long long)tokens * top_k <= teal::kMaxPairs;
+}
+
+size_t teal_workspace_bytes_arrange_experts(int experts, int pairs)
+{
+    if (experts < 1 || experts > TEAL_MAX_EXPERTS || pairs < 0 || pairs > teal::kMaxPairs) return 0;
+    const size_t bytes = teal::kCounterBytes + (size_t)teal::kMaxArrangeChunks * (experts + 1) * sizeof(int);
+    return (bytes + kAlignWorkspace - 1) / kAlignWorkspace * kAlignWorkspace;
+}
+
+teal_status teal_arrange_experts(const int32_t *idx, int tokens, int top_k, int experts, int32_t *order, int32_t *start,
+                                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!pairs_ok(tokens, top_k) || experts < 1 || experts > TEAL_MAX_EXPERTS) return TEAL_ERR_SHAPE;
+    if (!start || !workspace || (tokens > 0 && (!idx || !order))) return TEAL_ERR_NULL;
+    if (!aligned(idx, 4) || !aligned(order, 4) || !aligned(start, 4) || !aligned(workspace, kAlignWorkspace))
+        return TEAL_ERR_ALIGN;
+    if (workspace_bytes < teal_workspace_bytes_arrange_experts(experts, tokens * top_k)) return TEAL_ERR_WORKSPACE;
+    return from_hip(teal::launch_arrange_experts(idx, tokens, top_k, experts, order, start,
+                                                 ws_counters(workspace) + teal::kCounterBytes / sizeof(int),
+                                                 static_cast<hipStream_t>(stream)));
+}
+
+// What the grouped calls have in common; `multiple`: of the output width.
+static teal_status check_grouped(const teal::GroupedHostArgs &h, int multiple, int matrices)
+{
+    if (!pairs_ok(h.tokens, h.top_k) || h.experts < 1 || h.experts > TEAL_MAX_EXPERTS) return TEAL_ERR_SHAPE;
+    constexpr int kMaxWidth = 1 << 20;
+    if (h.m < 8 || h.m > kMaxWidth || h.m % 8 != 0 || h.n < multiple || h.n > kMaxWidth || h.n % multiple != 0)
+        return TEAL_ERR_SHAPE;
+    if ((long long)(h.tokens * h.top_k / 32 + h.experts) * ((h.n + 127) / 128) > kMaxTiles) return TEAL_ERR_SHAPE;
+    for (int k = 0; k < matrices; ++k)
+        if (!h.W[k] || (multiple == 32 && !h.scale[k])) return TEAL_ERR_NULL;
+    if (!h.start || (h.tokens > 0 && (!h.order || !h.rows || !h.out))) return TEAL_ERR_NULL;
+    for (int k = 0; k < matrices; ++k)
+        if (!aligned(h.W[k], 16) || !aligned(h.scale[k], 16)) return TEAL_ERR_ALIGN;
+    if (!aligned(h.order, 4) || !aligned(h.start, 4) || !aligned(h.rows, 16)) return TEAL_ERR_ALIGN;
+    return TEAL_OK;
+}
+
+static teal_status gate_up_call(const void *gate, const uint8_t *scale_gate, const void *up, const uint8_t *scale_up,
+                                int multiple, int experts, const int32_t *order, const int32_t *start, int tokens,
+                                int top_k, const void *X, void *H, int m, int f, void *stream)
+{
+    teal::GroupedHostArgs h{};
+    h.W[0] = gate;
+    h.W[1] = up;
+    h.scale[0] = scale_gate;
+    h.scale[1] = scale_up;
+    h.experts = experts;
+    h.tokens = tokens;
+    h.top_k = top_k;
+    h.order = order;
+    h.start = start;
+    h.rows = X;
+    h.out = H;
+    h.m = m;
+    h.n = f;
+    const teal_status st = check_grouped(h, multiple, 2);
+    if (st != TEAL_OK) return st;
+    if (!aligned(H, 16)) return TEAL_ERR_ALIGN;
+    if (tokens == 0) return TEAL_OK;
+    return from_hip(teal::launch_grouped_gate_up(h, static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_grouped_experts_bf16_gate_up(const void *Wt_gate, const void *Wt_up, int experts, const int32_t *order,
+                                              const int32_t *start, int tokens, int top_k, const void *X_bf16,
+                                              void *H_bf16, int m, int f, void *stream)
+{
+    return gate_up_call(Wt_gate, nullptr, Wt_up, nullptr, 8, experts, order, start, tokens, top_k, X_bf16, H_bf16, m, f,
+                        stream);
+}
+
+teal_status teal_grouped_experts_mx4_gate_up(const uint8_t *Wq_gate, const uint8_t *scale_gate, const uint8_t *Wq_up,
+                                             const uint8_t *scale_up, int experts, const int32_t *order,
+                                             const int32_t *start, int tokens, int top_k, const void *X_bf16,
+                                             void *H_bf16, int m, int f, void *stream)
+{
+    return gate_up_call(Wq_gate, scale_gate, Wq_up, scale_up, 32, experts, order, start, tokens, top_k, X_bf16, H_bf16, m,
+                        f, stream);
+}
+
+// A row of fp32 sums per pair, of as many columns at a time as take 512 MB (of 256 columns at least).
+static int grouped_slab_cols(int pairs, int n)
+{
+    const long long cols = (512ll << 20) / 4 / (pairs > 0 ? pairs : 1) / 256 * 256;
+    const int least = cols < 256 ? 256 : (int)(cols < teal::kMaxDim ? cols : teal::kMaxDim);
+    return least < n ? least : n;
+}
+
+size_t teal_workspace_bytes_grouped_experts(int pairs, int n)
+{
+    if (pairs < 0 || pairs > teal::kMaxPairs || n < 8 || n > 1 << 20) return 0;
+    const size_t bytes = teal::kCounterBytes + (size_t)pairs * grouped_slab_cols(pairs, n) * sizeof(float);
+    return (bytes + kAlignWorkspace - 1) / kAlignWorkspace * kAlignWorkspace;
+}
+
+static teal_status grouped_down_call(const void *W, const uint8_t *scale, int multiple, int experts,
+                                     const int32_t *order, const int32_t *start, int tokens, int top_k,
+                                     const int32_t *idx, const float *weight, const void *H, float *y, int m, int n,
+                                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    teal::GroupedHostArgs h{};
+    h.W[0] = W;
+    h.scale[0] = scale;
+    h.experts = experts;
+    h.tokens = tokens;
+    h.top_k = top_k;
+    h.order = order;
+    h.start = start;
+    h.idx = idx;
+    h.weight = weight;
+    h.rows = H;
+    h.out = y;
+    h.m = m;
+    h.n = n;
+    const teal_status st = check_grouped(h, multiple, 1);
+    if (st != TEAL_OK) return st;
+    if (!workspace || (tokens > 0 && (!idx || !weight))) return TEAL_ERR_NULL;
+    if (!aligned(idx, 4) || !aligned(weight, 4) || !aligned(y, 4) || !aligned(workspace, kAlignWorkspace))
+        return TEAL_ERR_ALIGN;
+    const int pairs = tokens * top_k;
+    if (workspace_bytes < teal_workspace_bytes_grouped_experts(pairs, n)) return TEAL_ERR_WORKSPACE;
+    if (tokens == 0) return TEAL_OK;
+    h.partial = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + teal::kCounterBytes);
+    h.slab_cols = grouped_slab_cols(pairs, n);
+    return from_hip(teal::launch_grouped_down(h, static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_grouped_experts_bf16_down(const void *Wt_down, int experts, const int32_t *order, const int32_t *start,
+                                           int tokens, int top_k, const int32_t *idx, const float *weight,
+                                           const void *H_bf16, float *y, int m, int n, void *workspace,
+                                           size_t workspace_bytes, void *stream)
+{
+    return grouped_down_call(Wt_down, nullptr, 8, experts, order, start, tokens, top_k, idx, weight, H_bf16, y, m, n,
+                             workspace, workspace_bytes, stream);
+}
+
+teal_status teal_grouped_experts_mx4_down(const uint8_t *Wq_down, const uint8_t *scale_down, int experts,
+                                          const int32_t *order, const int32_t *start, int tokens, int top_k,
+                                          const int32_t *idx, const float *weight, const void *H_bf16, float *y, int m,
+                                          int n, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return grouped_down_call(Wq_down, scale_down, 32, experts, order, start, tokens, top_k, idx, weight, H_bf16, y, m, n,
+                             workspace, workspace_bytes, stream);
+}
+
 teal_status teal_stream_read_probe(const void *buf, size_t bytes, int blocks, uint32_t match,
                                    uint32_t *sink, void *stream)
 {

@@ -201,6 +201,50 @@ struct RouteHostArgs {
 };
 hipError_t launch_route_experts(const RouteHostArgs &h, hipStream_t stream);
 
+// Products of many rows (gemm_w8.hip, grouped_experts.hip).
+constexpr int kMaxRowSum = 1 << 17;    // channels whose sum of products of 8-bit integers fits int32
+constexpr int kMaxPairs = 1 << 24;     // (token, expert) pairs of a grouped call
+__host__ __device__ constexpr int quantized_pitch(int m) { return (m + 127) / 128 * 128; }
+struct GemmShape {
+    int bm, bn;          // rows and columns of a block's tile
+    int splits;          // blocks along the sum
+};
+struct GemmW8HostArgs {
+    int count;
+    const int8_t *const *W;
+    const void *const *scale;
+    float *const *y;
+    const int *n;
+    const int8_t *Q;
+    const float *row_scale;
+    int rows, m;
+    int *counters, *partial;
+};
+hipError_t launch_quantize_rows(const void *X, bool bf16, int rows, int m, float t, int8_t *Q, float *scale,
+                                hipStream_t stream);
+hipError_t launch_quantize_rows_swiglu(const float *gate, const float *up, int rows, int m, float t, int8_t *Q,
+                                       float *scale, hipStream_t stream);
+hipError_t launch_gemm_w8(const GemmW8HostArgs &h, const GemmShape &sh, hipStream_t stream);
+
+struct GroupedHostArgs {
+    const void *W[2];              // of expert 0: gate and up, or W_down
+    const uint8_t *scale[2];       // microscaled weights, else NULL
+    int experts, tokens, top_k;
+    const int *order, *start;      // device: pairs in the experts' order, first place of each expert's
+    const int *idx;                // device [tokens][top_k]
+    const float *weight;
+    const void *rows;              // X [tokens][m] (gate and up) or H [tokens * top_k][m] (W_down), bf16
+    void *out;                     // H or y
+    int m, n;
+    float *partial;                // W_down: a row per pair
+    int slab_cols;                 // columns that it has room for
+};
+hipError_t launch_arrange_experts(const int *idx, int tokens, int top_k, int experts, int *order, int *start,
+                                  int *counts, hipStream_t stream);
+constexpr int kMaxArrangeChunks = 128;
+hipError_t launch_grouped_gate_up(const GroupedHostArgs &h, hipStream_t stream);
+hipError_t launch_grouped_down(const GroupedHostArgs &h, hipStream_t stream);
+
 // The MLP of a block in one launch (Appendix A.3): gate and up from x, then W_down on
 // SiLU(gate) . up, the blocks of W_down waiting for the gate / up tiles they read.
 struct MlpLaunch {
