@@ -629,7 +629,7 @@ teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *c
  *   X_bf16 [tokens][m] bf16 (the weights' type: a matrix instruction has one), H_bf16 [tokens * top_k][f] bf16, both
  *          16-byte aligned.
  *   m % 8 == 0, f % 8 == 0 (mx4: f % 32 == 0), 8 <= m, f <= 2^20, tokens * top_k as above, and
- *          (tokens * top_k / 32 + experts) * ceil(f / 128) <= 2^22 (else TEAL_ERR_SHAPE).
+ *          (tokens * top_k / 32 + experts) * ceil(f / 64) <= 2^22 (_down: ceil(n / 128); else TEAL_ERR_SHAPE).
  * teal_grouped_experts_{bf16,mx4}_down:
  *   y[b] = sum over j of weight[b][j] * (h W_down[e]^T), e = idx[b][j], h = the row of H that belongs to pair (b, j),
  * j ascending, in fp32.  A pair without an expert adds nothing, whatever its weight.

@@ -76,10 +76,12 @@ struct WeightsMx4 {
     typedef f32x4 Acc;
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// LOADERS wavefronts beside those that multiply do nothing but load (0: every wavefront loads its part).
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int LOADERS_ = 0>
 struct TileShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, LOADERS = LOADERS_;
+    static constexpr int kWaves = WM * WN, kThreads = 64 * (kWaves + LOADERS);
+    static constexpr int kLoadWaves = LOADERS > 0 ? LOADERS : kWaves;
     static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;       // 16 x 16 pieces of a wavefront
 };
 
@@ -94,17 +96,23 @@ struct TileProduct {
     static constexpr int kStage = kSlabX + (F::kMx4 ? kCodes + kScales : kSlabW);
     static constexpr int kRing = STAGES * kStage;
     static constexpr int kLds = kRing + (F::kMx4 ? 2 * kSlabW : 0);
-    static constexpr int kLoadsX = (BM / 8 + S::kWaves - 1) / S::kWaves;       // of 64 lanes x 16 bytes, a wavefront's
-    static constexpr int kLoadsW = F::kMx4 ? 2 : kSlabW / 1024 / S::kWaves;    // mx4: codes and scales
-    static constexpr int kRowsPerLoad = 1024 / kRowBytes;              // rows of W that a wavefront's load covers
-    static constexpr int kRowStep = kRowsPerLoad * S::kWaves;
+    static constexpr int kLoadWaves = S::kLoadWaves;
+    static constexpr int kLoadsX = (BM / 8 + kLoadWaves - 1) / kLoadWaves;     // of 64 lanes x 16 bytes, a wavefront's
+    static constexpr int kLoadsC = kCodes / 1024 / kLoadWaves;                 // mx4: of codes
+    static constexpr int kLoadsW = F::kMx4 ? kLoadsC + 1 : kSlabW / 1024 / kLoadWaves;
+    static constexpr int kRowsPerLoad = F::kMx4 ? 2048 / BN : 1024 / kRowBytes;     // rows of W that a load covers
+    static constexpr int kRowStep = kRowsPerLoad * kLoadWaves;
     static constexpr int kUnit = F::kBytes == 2 ? 32 : 16;             // bytes that a permutation keeps together
     static constexpr int kUnitMask = kRowBytes / HALVES / kUnit < 16 ? kRowBytes / HALVES / kUnit - 1 : 15;
     static constexpr int kHalfCols = BN / HALVES;
-    static_assert(BM % (16 * S::WM) == 0 && BN % (16 * S::WN) == 0 && kSlabW % (1024 * S::kWaves) == 0, "");
-    static_assert(!F::kMx4 || (kCodes == 16 * S::kThreads && S::kWaves >= HALVES), "a block of 32 codes per thread");
+    // A lane's permutation in its loads of W repeats with the bits of the row that it depends on.
+    static constexpr int kPeriod = F::kBytes == 2 ? 16 : 32;
+    static constexpr int kWLanes = F::kMx4 || kRowStep % kPeriod == 0 ? 1 : 2;
+    static_assert(BM % (16 * S::WM) == 0 && BN % (16 * S::WN) == 0 && kSlabW % (1024 * kLoadWaves) == 0, "");
+    static_assert(F::kMx4 || kWLanes * kRowStep % kPeriod == 0, "");
+    static_assert(!F::kMx4 || (kCodes == 16 * 64 * S::kWaves && kCodes % (1024 * kLoadWaves) == 0 && kLoadWaves >= HALVES),
+                  "a block of 32 codes per multiplying thread");
     static_assert(HALVES == 1 || NF % 2 == 0, "both matrices in every wavefront");
-    static_assert(kRowStep % 32 == 0 || (F::kBytes == 2 && kRowStep % 16 == 0), "a lane's permutation is the same in all its loads");
     static_assert(kLds <= 160 * 1024, "");
 
     typedef typename F::Acc Acc;
@@ -115,129 +123,169 @@ struct TileProduct {
         return (F::kBytes == 2 ? (k & 3) | (k >> 3 & 1) << 2 : (k & 7) | (k >> 4 & 1) << 3) & kUnitMask;
     }
 
+    // mx4: a unit's two chunks of 16 bytes change places every four channels, so that the lanes that write one of the two
+    // touch all banks.
+    static __device__ __forceinline__ int flip(int k) { return F::kMx4 ? (k >> 2 & 1) * 16 : 0; }
+
     unsigned lds;                                // of the ring
     int wave, lane, wm, wn;
+    int load_wave;                               // among those that load
     const unsigned char *x_lane[kLoadsX];        // this lane's chunk of its rows, first channel
-    const unsigned char *w_lane;                 // this lane's columns, its row of the first load, first channel of the sum
-    long long w_pitch;                           // bytes
+    const unsigned char *w_lane[kWLanes];        // this lane's columns, its row of the first loads, first channel of the sum
+    int w_pitch;                                 // bytes
     int x_chunk, w_row;                          // chunk of the row and row of the slab that the lane loads
-    // mx4: this lane's 16 bytes of scales, which come in tiles of 8 channels by 16 blocks; where the scale and the numbers
-    // of its codes are
+    // mx4: this lane's 16 bytes of scales, which come in tiles of 8 channels by 16 blocks; the row of the block that this
+    // thread converts, where its scale is and where its numbers go
     const unsigned char *s_lane;
     int s_pitch;                                 // bytes between tiles of one block row
+    int block_row;
     unsigned scale_at, value_at[4];
 
-    // `row_of(r)`: the address of the tile's row r of X (of any valid row where the tile has none).  `w_of(half)`: of the
-    // matrix; `scale_of(half)`: of its scales (mx4).  Columns from n on repeat the last ones (n a multiple of a chunk): they
-    // are not stored.
-    template <class RowOf, class WOf, class ScaleOf>
-    __device__ __forceinline__ void begin(void *smem, const RowOf &row_of, const WOf &w_of, const ScaleOf &scale_of,
-                                          int col0, int n)
+    __device__ __forceinline__ void begin(void *smem)
     {
         lds = lds_address(smem);
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wm = wave / S::WN;
         wn = wave % S::WN;
-        x_chunk = (lane & 7) ^ (lane >> 3);
-#pragma unroll
-        for (int j = 0; j < kLoadsX; ++j)
-            x_lane[j] = row_of(x_load(j) * 8 + (lane >> 3)) + 16 * x_chunk;
+        load_wave = S::LOADERS > 0 ? wave - S::kWaves : wave;
+    }
+    // Whether this wavefront multiplies and has a part of the result.
+    __device__ __forceinline__ bool multiplies() const { return S::LOADERS == 0 || wave < S::kWaves; }
+
+    __device__ __forceinline__ void begin_multiplying(int col0, int n)
+    {
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
             for (int f = 0; f < NF; ++f) acc[i][f] = Acc{};
-        const int at = (wave * 64 + lane) * 16;                        // in a slab
         if constexpr (F::kMx4) {
             constexpr int kBlocks = BN / 32 / HALVES;                  // of a row of one matrix
-            w_row = threadIdx.x / (BN / 32);
+            block_row = threadIdx.x / (BN / 32);
             const int half = threadIdx.x % (BN / 32) / kBlocks, in_half = threadIdx.x % kBlocks;
             const int col = min(col0 + 32 * in_half, n - 32);
-            w_pitch = n / 2;
-            w_lane = w_of(half) + w_row * w_pitch + col / 2;
-            // a wavefront loads the slab's scales of one matrix: lane / 8 the tile, lane % 8 the channel in it
-            s_pitch = mx4_scale_tiles(n) * kMx4TileBytes;
-            s_lane = scale_of(wave % HALVES) + (long long)(lane >> 3) * s_pitch + col0 / 512 * kMx4TileBytes + (lane & 7) * 16;
-            scale_at = kSlabX + kCodes + half * (kScales / HALVES) + (w_row / 8) * kMx4TileBytes + w_row % 8 * 16 + col / 32 % 16;
+            scale_at = kSlabX + kCodes + half * (kScales / HALVES) + (block_row / 8) * kMx4TileBytes + block_row % 8 * 16 +
+                       col / 32 % 16;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                value_at[q] = w_row * kRowBytes + half * (kRowBytes / HALVES) +
-                              ((2 * in_half + q / 2) ^ swizzle(w_row)) * 32 + q % 2 * 16;
+                value_at[q] = block_row * kRowBytes + half * (kRowBytes / HALVES) +
+                              ((2 * in_half + q / 2) ^ swizzle(block_row)) * 32 + (q % 2 * 16 ^ flip(block_row));
+        }
+    }
+
+    // `row_of(r)`: the address of the tile's row r of X (of any valid row where the tile has none).  `w_of(half)`: of the
+    // matrix; `scale_of(half)`: of its scales (mx4).  Columns from n on repeat the last ones (n a multiple of a chunk): they
+    // are not stored.
+    template <class RowOf, class WOf, class ScaleOf>
+    __device__ __forceinline__ void begin_loading(const RowOf &row_of, const WOf &w_of, const ScaleOf &scale_of, int col0,
+                                                  int n)
+    {
+        x_chunk = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+        for (int j = 0; j < kLoadsX; ++j) x_lane[j] = row_of(x_load(j) * 8 + (lane >> 3)) + 16 * x_chunk;
+        const int chunk = load_wave * 64 + lane;                       // of 16 bytes, in a slab of W
+        if constexpr (F::kMx4) {
+            constexpr int kBlocks = BN / 32 / HALVES;
+            w_row = chunk / (BN / 32);
+            const int half = chunk % (BN / 32) / kBlocks, in_half = chunk % kBlocks;
+            w_pitch = n / 2;
+            w_lane[0] = w_of(half) + (long long)w_row * w_pitch + min(col0 + 32 * in_half, n - 32) / 2;
+            // a wavefront loads the slab's scales of one matrix: lane / 8 the tile, lane % 8 the channel in it
+            s_pitch = mx4_scale_tiles(n) * kMx4TileBytes;
+            s_lane = scale_of(load_wave % HALVES) + (long long)(lane >> 3) * s_pitch + col0 / 512 * kMx4TileBytes +
+                     (lane & 7) * 16;
             return;
         }
+        const int at = chunk * 16;
         w_row = at / kRowBytes;
         const int half = HALVES == 1 ? 0 : at % kRowBytes / (kRowBytes / 2);
         const int in_half = at % (kRowBytes / HALVES);
-        const int unit = in_half / kUnit ^ swizzle(w_row);
-        const int col = min(col0 + (unit * kUnit + in_half % kUnit) / F::kBytes, n - 16 / F::kBytes);
-        w_pitch = (long long)n * F::kBytes;
-        w_lane = w_of(half) + w_row * w_pitch + (long long)col * F::kBytes;
+        w_pitch = n * F::kBytes;
+#pragma unroll
+        for (int v = 0; v < kWLanes; ++v) {
+            const int row = w_row + v * kRowStep;
+            const int unit = in_half / kUnit ^ swizzle(row);
+            const int col = min(col0 + (unit * kUnit + in_half % kUnit) / F::kBytes, n - 16 / F::kBytes);
+            w_lane[v] = w_of(half) + (long long)row * w_pitch + (long long)col * F::kBytes;
+        }
     }
     // Which 8 rows of X the wavefront's load j takes: where there are fewer loads than wavefronts some load the same.
-    __device__ __forceinline__ int x_load(int j) const { return (wave + j * S::kWaves) % (BM / 8); }
+    __device__ __forceinline__ int x_load(int j) const { return (load_wave + j * kLoadWaves) % (BM / 8); }
 
     // Slab `slab` of a sum of m channels into place `stage` of the ring: X, and W.  Channels from m on are zeros.
+    template <int LOADS>
     __device__ __forceinline__ void load_x(int slab, int stage, int m)
     {
         const unsigned to = lds + stage * kStage;
         const long long x_at = (long long)slab * kSlabBytes;
         const int k0 = slab * F::kSlabRows;
-        const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
         // (rows of 8-bit integers have zeros behind their end)
         if (F::kBytes == 1 || k0 + F::kSlabRows <= m) {
 #pragma unroll
-            for (int j = 0; j < kLoadsX; ++j) load_to_lds(x_lane[j] + x_at, to + x_load(j) * 1024);
+            for (int j = 0; j < LOADS; ++j) load_to_lds(x_lane[j] + x_at, to + x_load(j) * 1024);
         } else {
+            const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
             const bool in_row = k0 + x_chunk * (16 / F::kBytes) < m;
 #pragma unroll
-            for (int j = 0; j < kLoadsX; ++j) load_to_lds(in_row ? x_lane[j] + x_at : zero, to + x_load(j) * 1024);
+            for (int j = 0; j < LOADS; ++j) load_to_lds(in_row ? x_lane[j] + x_at : zero, to + x_load(j) * 1024);
         }
     }
     __device__ __forceinline__ void load_w(int slab, int stage, int m)
     {
-        const unsigned to = lds + stage * kStage + kSlabX + wave * 1024;
+        const unsigned to = lds + stage * kStage + kSlabX + load_wave * 1024;
+        const unsigned scales_to = lds + stage * kStage + kSlabX + kCodes + load_wave % HALVES * 1024;
+        constexpr int kLoads = F::kMx4 ? kLoadsC : kLoadsW;            // beside that of the scales
         const int k0 = slab * F::kSlabRows;
-        const unsigned char *const w_at = w_lane + k0 * w_pitch;
-        const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
-        if constexpr (F::kMx4) {
-            load_to_lds(k0 + w_row < m ? w_at : zero, to);
-            const unsigned char *const s_at = s_lane + (long long)(k0 / 8) * s_pitch;
-            load_to_lds(k0 + (lane & ~7) < m ? s_at : zero, lds + stage * kStage + kSlabX + kCodes + wave % HALVES * 1024);
-        } else if (k0 + F::kSlabRows <= m) {
+        const unsigned char *const s_at = F::kMx4 ? s_lane + (long long)(k0 / 8) * s_pitch : nullptr;
+        if (k0 + F::kSlabRows <= m) {
 #pragma unroll
-            for (int j = 0; j < kLoadsW; ++j) load_to_lds(w_at + j * kRowStep * w_pitch, to + j * S::kWaves * 1024);
+            for (int j = 0; j < kLoads; ++j) load_to_lds(w_at(k0, j), to + j * kLoadWaves * 1024);
+            if constexpr (F::kMx4) load_to_lds(s_at, scales_to);
         } else {
+            const unsigned char *const zero = reinterpret_cast<const unsigned char *>(&zero_chunk);
 #pragma unroll
-            for (int j = 0; j < kLoadsW; ++j)
-                load_to_lds(k0 + w_row + j * kRowStep < m ? w_at + j * kRowStep * w_pitch : zero,
-                            to + j * S::kWaves * 1024);
+            for (int j = 0; j < kLoads; ++j)
+                load_to_lds(k0 + w_row + j * kRowStep < m ? w_at(k0, j) : zero, to + j * kLoadWaves * 1024);
+            if constexpr (F::kMx4) load_to_lds(k0 + (lane & ~7) < m ? s_at : zero, scales_to);
         }
     }
+    // This lane's 16 bytes of load j of W, the slab from channel k0 on.
+    __device__ __forceinline__ const unsigned char *w_at(int k0, int j) const
+    {
+        return w_lane[j % kWLanes] + (long long)(k0 + j / kWLanes * kWLanes * kRowStep) * w_pitch;
+    }
 
-    // mx4: the codes of slab `slab` at `stage` of the ring to bf16 numbers in buffer `to`.
-    __device__ __forceinline__ void convert(int slab, int stage, int to, int m)
+    // mx4: this thread's block of 32 codes at `stage` of the ring and its scale, and those as bf16 numbers into buffer `to`.
+    struct Block {
+        u32x4 codes;
+        unsigned scale;
+    };
+    __device__ __forceinline__ Block read_block(int stage) const
     {
         typedef const __attribute__((address_space(3))) unsigned char *lds_ptr;
         typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
-        typedef __attribute__((address_space(3))) u32x4 *lds_out;
         const lds_ptr from = (lds_ptr)(uintptr_t)(lds + stage * kStage);
-        const u32x4 codes = *(lds_u32x4)(from + kSlabX + threadIdx.x * 16);
+        return {*(lds_u32x4)(from + kSlabX + threadIdx.x * 16), from[scale_at]};
+    }
+    __device__ __forceinline__ void convert(const Block &b, int slab, int to, int m)
+    {
+        typedef __attribute__((address_space(3))) u32x4 *lds_out;
         // what lies behind the last channel of a tile of scales has no meaning
-        const unsigned byte = slab * F::kSlabRows + w_row < m ? from[scale_at] : 0u;
-        const float sc = __uint_as_float(byte << 23);
+        const float sc = slab * F::kSlabRows + block_row < m ? __uint_as_float(b.scale << 23) : 0.f;
         const unsigned buffer = lds + kRing + to * kSlabW;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             u32x4 v;
-            v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 0));
-            v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 1));
-            v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 2));
-            v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[q], sc, 3));
+            v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 0));
+            v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 1));
+            v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 2));
+            v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 3));
             *(lds_out)(uintptr_t)(buffer + value_at[q]) = v;
         }
     }
 
-    // Multiplies in a slab whose X is at `x_at` and whose W is at `w_at` in LDS.
+    // Multiplies in a slab whose X is at `x_at` and whose W is at `w_at` in LDS; the first LIVE pieces of rows.
+    template <int LIVE>
     __device__ __forceinline__ void multiply(unsigned x_at, unsigned w_at)
     {
         typedef const __attribute__((address_space(3))) unsigned char *lds_ptr;
@@ -255,10 +303,11 @@ struct TileProduct {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
                     typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
                     const int k = 32 * ks + 8 * g + l / 4;             // and 4 further
-                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 + l % 4 * 8;
+                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 + l % 4 * 8;      // flip(k) is 0
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
-                    const uint2 b = __builtin_bit_cast(
-                        uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * kRowBytes)));
+                    const lds_ptr p4 = w + (k + 4) * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 +
+                                       (l % 4 * 8 ^ flip(4));
+                    const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p4));
                     W[f] = u32x4{a.x, a.y, b.x, b.y};
                 } else {
                     typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -272,8 +321,8 @@ struct TileProduct {
                 }
             }
 #pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                const int row = (wm * MF + i) * 16 + l;
+            for (int i = 0; i < LIVE; ++i) {
+                const int row = (i * S::WM + wm) * 16 + l;
                 const u32x4 X = *(lds_u32x4)(x + row * kSlabBytes + ((4 * ks + g) ^ (l & 7)) * 16);
 #pragma unroll
                 for (int f = 0; f < NF; ++f) {
@@ -288,44 +337,82 @@ struct TileProduct {
         }
     }
 
-    // Slabs [first, last) of a sum of m channels.
-    __device__ __forceinline__ void run(int first, int last, int m)
+    // Slabs [first, last) of a sum of m channels, for the first `rows` rows of the tile: a tile that is a
+    // quarter, half or three quarters empty multiplies (and loads) only the others of its pieces.
+    __device__ __forceinline__ void run(int first, int last, int m, int rows)
     {
-        constexpr int kLoads = kLoadsX + kLoadsW;
+        if constexpr (MF >= 4) {
+            if (rows <= BM / 4) return run_pieces<MF / 4>(first, last, m);
+            if (rows <= BM / 2) return run_pieces<MF / 2>(first, last, m);
+            if constexpr (MF >= 8)
+                if (rows <= BM / 4 * 3) return run_pieces<MF / 4 * 3>(first, last, m);
+        }
+        run_pieces<MF>(first, last, m);
+    }
+    template <int LIVE>
+    __device__ __forceinline__ void run_pieces(int first, int last, int m)
+    {
+        constexpr int kPieceLoads = LIVE * S::WM * 2 / kLoadWaves;
+        constexpr int kLiveX = kPieceLoads < 1 ? 1 : kPieceLoads;
+        constexpr int kLoads = kLiveX + kLoadsW;
         constexpr int kAhead = F::kMx4 ? 1 : 0;          // by how many slabs W is ahead of X
+        const bool loads = S::LOADERS == 0 || !multiplies();
         if constexpr (F::kMx4) {
-            load_w(first, STAGES - 1, m);
+            if (loads) load_w(first, STAGES - 1, m);
             wait_and_meet<0>();
-            convert(first, STAGES - 1, 0, m);      // (the place is filled again after the next meeting)
+            if (multiplies()) convert(read_block(STAGES - 1), first, 0, m);      // (the place is filled after the next meeting)
         }
         // Place s of the ring: X of slab first + s, and W of the same slab (mx4: of the next one).
+        if (loads) {
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) {
-            if (first + s < last) load_x(first + s, s, m);
-            if (first + s + kAhead < last) load_w(first + s + kAhead, s, m);
+            for (int s = 0; s < STAGES - 1; ++s) {
+                if (first + s < last) load_x<kLiveX>(first + s, s, m);
+                if (first + s + kAhead < last) load_w(first + s + kAhead, s, m);
+            }
         }
-        int stage = 0, buffer = 0;
-        for (int slab = first; slab < last; ++slab) {
-            // what later slabs loaded may still be under way
+        // Before slab `slab`: what later slabs loaded may still be under way.
+        auto meet = [&](int slab) {
             if (slab + STAGES - 2 + kAhead < last)
                 wait_and_meet<(STAGES - 2) * kLoads>();
             else
                 wait_and_meet<0>();
+        };
+        auto load_next = [&](int slab, int stage) {
             const int next = slab + STAGES - 1, to = stage == 0 ? STAGES - 1 : stage - 1;
-            if (next < last) load_x(next, to, m);
+            if (next < last) load_x<kLiveX>(next, to, m);
             if (next + kAhead < last) load_w(next + kAhead, to, m);
+        };
+        int stage = 0, buffer = 0;
+        if (S::LOADERS > 0 && !multiplies()) {
+            for (int slab = first; slab < last; ++slab) {
+                meet(slab);
+                load_next(slab, stage);
+                stage = stage == STAGES - 1 ? 0 : stage + 1;
+            }
+            return;
+        }
+        for (int slab = first; slab < last; ++slab) {
+            if constexpr (S::LOADERS > 0) {
+                wait_and_meet<0>();                      // (of LDS operations: there are no others)
+            } else {
+                meet(slab);
+                load_next(slab, stage);
+            }
             const unsigned x_at = lds + stage * kStage;
-            multiply(x_at, F::kMx4 ? lds + kRing + buffer * kSlabW : x_at + kSlabX);
             if constexpr (F::kMx4) {
-                if (slab + 1 < last) convert(slab + 1, stage, buffer ^ 1, m);
+                const Block block = read_block(stage);         // (past the last slab: what is there)
+                multiply<LIVE>(x_at, lds + kRing + buffer * kSlabW);
                 buffer ^= 1;
+                if (slab + 1 < last) convert(block, slab + 1, buffer, m);
+            } else {
+                multiply<LIVE>(x_at, x_at + kSlabX);
             }
             stage = stage == STAGES - 1 ? 0 : stage + 1;
         }
     }
 
     // Row of the tile and first of four neighbouring columns (of a half) that acc[i][f] holds.
-    __device__ __forceinline__ int row_of(int i) const { return (wm * MF + i) * 16 + (lane & 15); }
+    __device__ __forceinline__ int row_of(int i) const { return (i * S::WM + wm) * 16 + (lane & 15); }
     __device__ __forceinline__ int col_of(int f) const
     {
         const int piece = HALVES == 1 ? wn * NF + f : wn * (NF / 2) + f % (NF / 2);

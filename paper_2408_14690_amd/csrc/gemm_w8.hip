@@ -205,49 +205,68 @@ __global__ __launch_bounds__(S::kThreads) void gemm_w8_kernel(GemmW8Args a)
     const int col0 = (gtile - first) * S::BN;
 
     Product p;
-    p.begin(smem,
+    p.begin(smem);
+    if (p.multiplies()) p.begin_multiplying(col0, n);
+    if (S::LOADERS == 0 || !p.multiplies())
+        p.begin_loading(
             [&](int r) {
                 return reinterpret_cast<const unsigned char *>(a.Q) + (size_t)min(row0 + r, a.rows - 1) * a.pitch;
             },
-            [&](int) { return reinterpret_cast<const unsigned char *>(W); },
-            [](int) { return nullptr; }, col0, n);
+            [&](int) { return reinterpret_cast<const unsigned char *>(W); }, [](int) { return nullptr; }, col0, n);
     const int slabs = a.pitch / kSlabBytes;
     const int slab0 = split * a.slabs_per_split;
-    p.run(slab0, min(slabs, slab0 + a.slabs_per_split), a.m);
+    p.run(slab0, min(slabs, slab0 + a.slabs_per_split), a.m, a.rows - row0);
 
-    if (a.splits > 1) {
+    // (tiles of more rows are not sliced)
+    if (S::BM <= kMaxSlicedRows && a.splits > 1) {
         // Every slice leaves its sums, and the last one of a tile to arrive adds the others' to its own: whole numbers, in any
         // order the same.
-        constexpr int kPieces = S::MF * S::NF;
+        constexpr int kPieces = S::MF * S::NF, kOwners = 64 * S::kWaves;
         const Buffer sums = buffer_of(a.partial + (size_t)place * a.splits * (S::BM * S::BN),
                                       4u * a.splits * (S::BM * S::BN));
+        if (p.multiplies()) {
 #pragma unroll
-        for (int i = 0; i < S::MF; ++i)
+            for (int i = 0; i < S::MF; ++i)
 #pragma unroll
-            for (int f = 0; f < S::NF; ++f)
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p.acc[i][f]), sums,
-                                                       16 * (int)threadIdx.x,
-                                                       16 * S::kThreads * (split * kPieces + i * S::NF + f), kAgentScope);
-        wait_vector_memory();
+                for (int f = 0; f < S::NF; ++f)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p.acc[i][f]), sums,
+                                                           16 * (int)threadIdx.x,
+                                                           16 * kOwners * (split * kPieces + i * S::NF + f), kAgentScope);
+            wait_vector_memory();
+        }
         __syncthreads();
         if (threadIdx.x == 0)
             arrived = __hip_atomic_fetch_add(a.counters + place, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
-        if (arrived != a.splits - 1) return;
+        if (arrived != a.splits - 1 || !p.multiplies()) return;
         if (threadIdx.x == 0) store_coherent(a.counters + place, 0);
-        for (int s = 0; s < a.splits; ++s) {
-            if (s == split) continue;
+        // 16 loads on their way together: one after the other each would take a trip to memory
+        constexpr int kBatch = kPieces < 16 ? kPieces : 16, kTogether = 16 / kBatch;
+        for (int s0 = 0; s0 < a.splits; s0 += kTogether) {
 #pragma unroll
-            for (int i = 0; i < S::MF; ++i)
+            for (int q0 = 0; q0 < kPieces; q0 += kBatch) {
+                u32x4 other[kTogether][kBatch];
 #pragma unroll
-                for (int f = 0; f < S::NF; ++f) {
-                    const u32x4 other = __builtin_amdgcn_raw_buffer_load_b128(
-                        sums, 16 * (int)threadIdx.x, 16 * S::kThreads * (s * kPieces + i * S::NF + f), kAgentScope);
-                    p.acc[i][f] += __builtin_bit_cast(i32x4, other);
+                for (int t = 0; t < kTogether; ++t)
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q)
+                        other[t][q] = __builtin_amdgcn_raw_buffer_load_b128(
+                            sums, 16 * (int)threadIdx.x,
+                            16 * kOwners * (min(s0 + t, a.splits - 1) * kPieces + q0 + q), kAgentScope);
+#pragma unroll
+                for (int t = 0; t < kTogether; ++t) {
+                    const int take = s0 + t < a.splits && s0 + t != split ? -1 : 0;
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            p.acc[(q0 + q) / S::NF][(q0 + q) % S::NF][r] += (int)other[t][q][r] & take;
                 }
+            }
         }
     }
 
+    if (!p.multiplies()) return;
 #pragma unroll
     for (int f = 0; f < S::NF; ++f) {
         const int col = col0 + p.col_of(f);
@@ -270,10 +289,6 @@ __global__ __launch_bounds__(S::kThreads) void gemm_w8_kernel(GemmW8Args a)
         }
     }
 }
-
-typedef TileShape<256, 256, 2, 4, 2> Large;
-typedef TileShape<128, 128, 2, 2, 2> Medium;
-typedef TileShape<32, 128, 1, 4, 4> Few;
 
 template <class S>
 hipError_t launch(const GemmW8Args &a, hipStream_t stream)
@@ -339,9 +354,15 @@ hipError_t launch_gemm_w8(const GemmW8HostArgs &h, const GemmShape &sh, hipStrea
     a.splits = (slabs + a.slabs_per_split - 1) / a.slabs_per_split;      // none of them empty
     a.counters = h.counters;
     a.partial = h.partial;
-    if (sh.bm == 256) return launch<Large>(a, stream);
-    if (sh.bm == 128) return launch<Medium>(a, stream);
-    return launch<Few>(a, stream);
+    switch (sh.bm) {
+    case 16: return launch<TileShape<16, 128, 1, 4, 4, 2>>(a, stream);
+    case 32: return launch<TileShape<32, 128, 1, 4, 3, 4>>(a, stream);
+    case 64: return launch<TileShape<64, 128, 1, 4, 3, 4>>(a, stream);
+    case 128: return launch<TileShape<128, 128, 2, 4, 4, 4>>(a, stream);
+    default:
+        return sh.bn == 128 ? launch<TileShape<256, 128, 4, 2, 3, 4>>(a, stream)
+                            : launch<TileShape<256, 256, 2, 4, 2, 4>>(a, stream);
+    }
 }
 
 }  // namespace teal

@@ -3,6 +3,8 @@
 #include "gemm_tile.h"
 #include "teal_internal.h"
 
+#include <cmath>
+
 namespace teal {
 
 namespace {
@@ -79,10 +81,17 @@ __global__ __launch_bounds__(kArrangeThreads) void place_pairs_kernel(ArrangeArg
         if constexpr (ALONE) {
             for (int v = 0; v < kArrangeWaves; ++v) total += at[v][e];
         } else {
-            for (int c = 0; c < (int)gridDim.x; ++c) {
-                const int n = a.counts[c * keys + e];
-                total += n;
-                before += c < (int)blockIdx.x ? n : 0;
+            // several on their way together: one after the other each would take a trip to memory
+            const int chunks = gridDim.x;
+            for (int c0 = 0; c0 < chunks; c0 += 32) {
+                int n[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) n[c] = a.counts[min(c0 + c, chunks - 1) * keys + e];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                    total += c0 + c < chunks ? n[c] : 0;
+                    before += c0 + c < (int)blockIdx.x ? n[c] : 0;
+                }
             }
         }
     }
@@ -212,13 +221,17 @@ __global__ __launch_bounds__(S::kThreads) void grouped_gate_up_kernel(GroupedArg
     if (!find_tile<S::BM>(a, t)) return;
     const int col0 = a.col_begin + t.col_tile * (S::BN / 2);
     Product p;
-    p.begin(smem,
+    p.begin(smem);
+    if (p.multiplies()) p.begin_multiplying(col0, a.n);
+    if (S::LOADERS == 0 || !p.multiplies())
+        p.begin_loading(
             [&](int r) {
                 return a.rows + (size_t)(pair_at(a, min(t.row0 + r, t.row_end - 1)) / a.top_k) * (2 * (size_t)a.m);
             },
             [&](int half) { return a.W[half] + t.expert * expert_bytes<F>(a.m, a.n); },
             [&](int half) { return a.scale[half] + t.expert * mx4_scale_bytes(a.m, a.n); }, col0, a.n);
-    p.run(0, (a.m + F::kSlabRows - 1) / F::kSlabRows, a.m);
+    p.run(0, (a.m + F::kSlabRows - 1) / F::kSlabRows, a.m, t.row_end - t.row0);
+    if (!p.multiplies()) return;
 #pragma unroll
     for (int f = 0; f < S::NF / 2; ++f) {
         const int col = col0 + p.col_of(f);
@@ -247,10 +260,14 @@ __global__ __launch_bounds__(S::kThreads) void grouped_down_kernel(GroupedArgs a
     if (!find_tile<S::BM>(a, t)) return;
     const int col0 = a.col_begin + t.col_tile * S::BN;
     Product p;
-    p.begin(smem, [&](int r) { return a.rows + (size_t)min(t.row0 + r, t.row_end - 1) * (2 * (size_t)a.m); },
-            [&](int) { return a.W[0] + t.expert * expert_bytes<F>(a.m, a.n); },
-            [&](int) { return a.scale[0] + t.expert * mx4_scale_bytes(a.m, a.n); }, col0, a.n);
-    p.run(0, (a.m + F::kSlabRows - 1) / F::kSlabRows, a.m);
+    p.begin(smem);
+    if (p.multiplies()) p.begin_multiplying(col0, a.n);
+    if (S::LOADERS == 0 || !p.multiplies())
+        p.begin_loading([&](int r) { return a.rows + (size_t)min(t.row0 + r, t.row_end - 1) * (2 * (size_t)a.m); },
+                        [&](int) { return a.W[0] + t.expert * expert_bytes<F>(a.m, a.n); },
+                        [&](int) { return a.scale[0] + t.expert * mx4_scale_bytes(a.m, a.n); }, col0, a.n);
+    p.run(0, (a.m + F::kSlabRows - 1) / F::kSlabRows, a.m, t.row_end - t.row0);
+    if (!p.multiplies()) return;
 #pragma unroll
     for (int i = 0; i < S::MF; ++i) {
         const int row = t.row0 + p.row_of(i);
@@ -286,9 +303,6 @@ __global__ __launch_bounds__(256) void join_pairs_kernel(const float *partial, c
     for (int r = 0; r < 4; ++r) to[r] = sum[r];
 }
 
-typedef TileShape<256, 256, 2, 4, 2> Large;
-typedef TileShape<64, 256, 1, 8, 2> Small;
-
 // Blocks for all row tiles that the experts' pairs can make, times the column tiles.
 unsigned grid_of(const GroupedArgs &a, int bm)
 {
@@ -315,36 +329,38 @@ GroupedArgs grouped_args(const GroupedHostArgs &h)
     return a;
 }
 
-bool many_rows(const GroupedHostArgs &h) { return (long long)h.tokens * h.top_k > 128ll * h.experts; }
-
 template <class F, class S>
-hipError_t gate_up(const GroupedHostArgs &h, hipStream_t stream)
-{
-    GroupedArgs a = grouped_args(h);
-    a.out = h.out;
-    a.col_tiles = (h.n + S::BN / 2 - 1) / (S::BN / 2);
-    hipLaunchKernelGGL((grouped_gate_up_kernel<F, S>), dim3(grid_of(a, S::BM)), dim3(S::kThreads), 0, stream, a);
-    return hipGetLastError();
-}
-
-template <class F, class S>
-hipError_t down(const GroupedHostArgs &h, hipStream_t stream)
-{
-    GroupedArgs a = grouped_args(h);
-    a.out = h.partial;
-    for (int col = 0; col < h.n; col += h.slab_cols) {
-        const int cols = h.n - col < h.slab_cols ? h.n - col : h.slab_cols;
-        a.col_begin = col;
-        a.out_pitch = cols;
-        a.col_tiles = (cols + S::BN - 1) / S::BN;
-        hipLaunchKernelGGL((grouped_down_kernel<F, S>), dim3(grid_of(a, S::BM)), dim3(S::kThreads), 0, stream, a);
-        const long long threads = (long long)h.tokens * (cols / 4);
-        hipLaunchKernelGGL(join_pairs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, h.partial,
-                           h.idx, h.weight, h.tokens, h.top_k, h.experts, cols / 4, cols, static_cast<float *>(h.out),
-                           h.n, col);
+struct GateUp {
+    static hipError_t run(const GroupedHostArgs &h, hipStream_t stream)
+    {
+        GroupedArgs a = grouped_args(h);
+        a.out = h.out;
+        a.col_tiles = (h.n + S::BN / 2 - 1) / (S::BN / 2);
+        hipLaunchKernelGGL((grouped_gate_up_kernel<F, S>), dim3(grid_of(a, S::BM)), dim3(S::kThreads), 0, stream, a);
+        return hipGetLastError();
     }
-    return hipGetLastError();
-}
+};
+
+template <class F, class S>
+struct Down {
+    static hipError_t run(const GroupedHostArgs &h, hipStream_t stream)
+    {
+        GroupedArgs a = grouped_args(h);
+        a.out = h.partial;
+        for (int col = 0; col < h.n; col += h.slab_cols) {
+            const int cols = h.n - col < h.slab_cols ? h.n - col : h.slab_cols;
+            a.col_begin = col;
+            a.out_pitch = cols;
+            a.col_tiles = (cols + S::BN - 1) / S::BN;
+            hipLaunchKernelGGL((grouped_down_kernel<F, S>), dim3(grid_of(a, S::BM)), dim3(S::kThreads), 0, stream, a);
+            const long long threads = (long long)h.tokens * (cols / 4);
+            hipLaunchKernelGGL(join_pairs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, h.partial,
+                               h.idx, h.weight, h.tokens, h.top_k, h.experts, cols / 4, cols, static_cast<float *>(h.out),
+                               h.n, col);
+        }
+        return hipGetLastError();
+    }
+};
 
 }  // namespace
 
@@ -367,16 +383,66 @@ hipError_t launch_arrange_experts(const int *idx, int tokens, int top_k, int exp
     return hipGetLastError();
 }
 
+namespace {
+
+// Shape of the tiles, by the rows that an expert has on average (r).  Few rows: what counts is that W is read once and much
+// of it at a time, two blocks on a compute unit.  Many: the tiles that load least for what they multiply, as long as
+// they fill the units; compared by the rounds of tiles that the units take and the time of a slab (us, measured on
+// full launches), the last tile of an expert taken as half empty.  What was measured (us, gate and up / down):
+//   bf16, 64 tokens, 2 of 8 experts of 4096 -> 14336 (r = 16)      32 x 128 347 / 185, 64 x 128 348 / 160, 128 x 256 346 / 179
+//   256 tokens of the same (r = 64)       64 x 128 447 / 239, 128 x 128 415 / 185, 128 x 256 380 / 213, 256 x 256 416 / 289
+//   2048 tokens (r = 512)                 128 x 128 1313 / 691, 128 x 256 1010 / 603, 256 x 256 1013 / 667
+//   8192 tokens (r = 2048)                128 x 256 3753 / 2040, 256 x 256 3537 / 2043
+//   4096 tokens, 8 of 128 experts of 2048 -> 768 (r = 256)         128 x 128 334 / 308, 128 x 256 264 / 260, 256 x 256 275 / 257
+//   mx4, where every block converts what it reads: r = 4 32 x 128 169 / 90, 64 x 128 slower; r = 64 64 x 128 281 / 181,
+//   128 x 256 315 / 294; r = 512 64 x 128 1472 / 782, 256 x 128 1239 / 672, 256 x 256 1168 / 845
+struct GroupedShape {
+    int bm, bn;
+};
+GroupedShape grouped_shape(const GroupedHostArgs &h, int cols)
+{
+    const bool mx4 = h.scale[0] != nullptr;
+    const long long pairs = (long long)h.tokens * h.top_k;
+    const double experts = pairs < h.experts ? (double)pairs : (double)h.experts, r = pairs / experts;
+    if (r <= 8) return {32, 128};
+    if (r <= (mx4 ? 128 : 32)) return {64, 128};
+    auto time = [&](int bm, int bn, double slab) {
+        const double tiles = r <= bm / 2 ? experts : experts * (r / bm + 0.5);
+        return std::ceil(tiles * ((cols + bn - 1) / bn) / 256) * slab;
+    };
+    if (mx4) return {256, time(256, 128, 1.1) < time(256, 256, 1.85) ? 128 : 256};
+    const double narrow = time(128, 128, 0.65), wide = time(128, 256, 1.0), large = time(256, 256, 1.85);
+    if (large < wide && large < narrow) return {256, 256};
+    return {128, narrow < wide ? 128 : 256};
+}
+
+template <template <class, class> class Call>
+hipError_t run_grouped(const GroupedHostArgs &h, GroupedShape s, hipStream_t stream)
+{
+    if (h.scale[0]) {
+        if (s.bm == 32) return Call<WeightsMx4, TileShape<32, 128, 1, 4, 4, 4>>::run(h, stream);
+        if (s.bm == 64) return Call<WeightsMx4, TileShape<64, 128, 1, 4, 3, 4>>::run(h, stream);
+        // (with wavefronts that load beside them those of 256 x 256 would have 168 registers each: 1240 us where 1168)
+        return s.bn == 128 ? Call<WeightsMx4, TileShape<256, 128, 4, 1, 3, 4>>::run(h, stream)
+                           : Call<WeightsMx4, TileShape<256, 256, 2, 4, 2>>::run(h, stream);
+    }
+    if (s.bm == 32) return Call<WeightsBf16, TileShape<32, 128, 1, 4, 3, 4>>::run(h, stream);
+    if (s.bm == 64) return Call<WeightsBf16, TileShape<64, 128, 1, 4, 3, 4>>::run(h, stream);
+    if (s.bm == 256) return Call<WeightsBf16, TileShape<256, 256, 2, 4, 2>>::run(h, stream);
+    return s.bn == 128 ? Call<WeightsBf16, TileShape<128, 128, 2, 4, 4, 4>>::run(h, stream)
+                       : Call<WeightsBf16, TileShape<128, 256, 2, 4, 3, 4>>::run(h, stream);
+}
+
+}  // namespace
+
 hipError_t launch_grouped_gate_up(const GroupedHostArgs &h, hipStream_t stream)
 {
-    if (h.scale[0]) return many_rows(h) ? gate_up<WeightsMx4, Large>(h, stream) : gate_up<WeightsMx4, Small>(h, stream);
-    return many_rows(h) ? gate_up<WeightsBf16, Large>(h, stream) : gate_up<WeightsBf16, Small>(h, stream);
+    return run_grouped<GateUp>(h, grouped_shape(h, 2 * h.n), stream);
 }
 
 hipError_t launch_grouped_down(const GroupedHostArgs &h, hipStream_t stream)
 {
-    if (h.scale[0]) return many_rows(h) ? down<WeightsMx4, Large>(h, stream) : down<WeightsMx4, Small>(h, stream);
-    return many_rows(h) ? down<WeightsBf16, Large>(h, stream) : down<WeightsBf16, Small>(h, stream);
+    return run_grouped<Down>(h, grouped_shape(h, h.n), stream);
 }
 
 }  // namespace teal

@@ -1513,31 +1513,62 @@ teal_status teal_quantize_rows_swiglu(const float *gate, const float *up, int ro
                                                       static_cast<hipStream_t>(stream)));
 }
 
-// Shape of the products of `rows` rows with matrices of widths n.
+// Shape of the products of `rows` rows with matrices of widths n: the least estimated time.  A slab (128 channels) of a tile
+// takes a compute unit `alone` microseconds with one block on it, `pair` with two (0: LDS has no room for two), measured on
+// full launches (4096 x 8192 -> 28672 rows in 256 x 256 tiles 7 x 64 slabs in 840 us, 2048 x 14336 -> 4096 in 256 x 128 112
+// in 120; 333 x 5001 -> 3840 in 128 x 128 20 in 14 beside what the launch's ends take, in 64 x 128 40 in 17).  Weights come
+// from memory at 4.6 TB/s and all that the tiles load from the caches at 12.  Slices take 2 us more and their sums' way to memory and back at 4.5 TB/s, to the
+// one block that adds a tile's at 0.1.
+struct GemmTiles {
+    int bm, bn;
+    double alone, pair;
+};
+static constexpr GemmTiles kGemmTiles[] = {{16, 128, 0.22, 0.60}, {32, 128, 0.28, 0.50}, {64, 128, 0.36, 0.85},
+                                           {128, 128, 0.52, 0.0}, {256, 128, 1.00, 0.0}, {256, 256, 1.82, 0.0}};
+static constexpr int kUnits = 256, kMaxSlicedBlocks = 512;
+
 static teal::GemmShape gemm_w8_shape(int rows, int m, const int *n, int count)
 {
-    auto col_tiles = [&](int bn) {
-        long long tiles = 0;
-        for (int k = 0; k < count; ++k) tiles += (n[k] + bn - 1) / bn;
-        return tiles;
-    };
-    teal::GemmShape s{256, 256, 1};
-    if (rows <= 64) s = {32, 128, 1};
-    else if (rows <= 512 || (long long)((rows + 255) / 256) * col_tiles(256) < 192) s = {128, 128, 1};
-    const long long tiles = (long long)((rows + s.bm - 1) / s.bm) * col_tiles(s.bn);
     const int slabs = teal::quantized_pitch(m) / 128;
-    if (s.bm < 256)
-        while (tiles * s.splits * 2 <= 512 && slabs >= s.splits * 2) s.splits *= 2;
-    return s;
+    double least = 0.0, bytes = 0.0;
+    for (int k = 0; k < count; ++k) bytes += (double)n[k] * m;
+    teal::GemmShape best{256, 256, 1};
+    for (const GemmTiles &t : kGemmTiles) {
+        if (t.bm > 16 && t.bm >= 2 * rows) break;              // half of it or more would be empty
+        long long tiles = 0;
+        for (int k = 0; k < count; ++k) tiles += (n[k] + t.bn - 1) / t.bn;
+        tiles *= (rows + t.bm - 1) / t.bm;
+        for (int splits = 1; splits <= 16 && splits <= slabs; ++splits) {
+            const long long blocks = tiles * splits;
+            if (splits > 1 && (blocks > kMaxSlicedBlocks || t.bm > teal::kMaxSlicedRows)) break;
+            const long long resident = t.pair > 0 ? 2 * kUnits : kUnits, rest = blocks % resident;
+            const double full = t.pair > 0 ? t.pair : t.alone;
+            const double round = blocks / resident * full + (rest == 0 ? 0.0 : rest <= kUnits ? t.alone : full);
+            double time = round * ((slabs + splits - 1) / splits);
+            if (time < bytes / 4.6e6) time = bytes / 4.6e6;
+            const double loaded = (double)tiles * slabs * (t.bm + t.bn) * 128, tile_bytes = 4.0 * t.bm * t.bn;
+            if (time < loaded / 12e6) time = loaded / 12e6;
+            time += loaded / 100e6;                            // of equal ones the one that loads less
+            if (splits > 1) {
+                const double one = splits * tile_bytes / 1e5, all = 2 * blocks * tile_bytes / 4.5e6;
+                time += 2.0 + (one > all ? one : all);
+            }
+            if (least == 0.0 || time < least) {
+                least = time;
+                best = {t.bm, t.bn, splits};
+            }
+        }
+    }
+    return best;
 }
-
-// Sums of the slices: of at most 512 blocks.
-static constexpr size_t kGemmPartialBytes = 512 * (size_t)(128 * 128 * 4);
 
 size_t teal_workspace_bytes_gemm_w8(int rows, int m, int n)
 {
     if (rows < 0 || rows > TEAL_MAX_ROWS || m < 1 || m > TEAL_MAX_ROW_SUM || n < 16 || n > teal::kMaxDim) return 0;
-    return teal::kCounterBytes + kGemmPartialBytes;
+    // the sums of the slices: tiles of at most 128 rows, the smallest that has all of them or the next larger
+    int bm = 16;
+    while (bm < teal::kMaxSlicedRows && bm < 2 * rows) bm *= 2;
+    return teal::kCounterBytes + (size_t)kMaxSlicedBlocks * bm * 128 * sizeof(int);
 }
 
 teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
@@ -1604,7 +1635,8 @@ static teal_status check_grouped(const teal::GroupedHostArgs &h, int multiple, i
     constexpr int kMaxWidth = 1 << 20;
     if (h.m < 8 || h.m > kMaxWidth || h.m % 8 != 0 || h.n < multiple || h.n > kMaxWidth || h.n % multiple != 0)
         return TEAL_ERR_SHAPE;
-    if ((long long)(h.tokens * h.top_k / 32 + h.experts) * ((h.n + 127) / 128) > kMaxTiles) return TEAL_ERR_SHAPE;
+    const long long cols = (long long)h.n * matrices;
+    if ((h.tokens * h.top_k / 32 + h.experts) * ((cols + 127) / 128) > kMaxTiles) return TEAL_ERR_SHAPE;
     for (int k = 0; k < matrices; ++k)
         if (!h.W[k] || (multiple == 32 && !h.scale[k])) return TEAL_ERR_NULL;
     if (!h.start || (h.tokens > 0 && (!h.order || !h.rows || !h.out))) return TEAL_ERR_NULL;
@@ -1656,10 +1688,10 @@ teal_status teal_grouped_experts_mx4_gate_up(const uint8_t *Wq_gate, const uint8
                         f, stream);
 }
 
-// A row of fp32 sums per pair, of as many columns at a time as take 512 MB (of 256 columns at least).
+// A row of fp32 sums per pair, of as many columns at a time as take 256 MB (of 256 columns at least).
 static int grouped_slab_cols(int pairs, int n)
 {
-    const long long cols = (512ll << 20) / 4 / (pairs > 0 ? pairs : 1) / 256 * 256;
+    const long long cols = (256ll << 20) / 4 / (pairs > 0 ? pairs : 1) / 256 * 256;
     const int least = cols < 256 ? 256 : (int)(cols < teal::kMaxDim ? cols : teal::kMaxDim);
     return least < n ? least : n;
 }

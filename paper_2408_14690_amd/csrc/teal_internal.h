@@ -209,6 +209,7 @@ struct GemmShape {
     int bm, bn;          // rows and columns of a block's tile
     int splits;          // blocks along the sum
 };
+constexpr int kMaxSlicedRows = 128;    // of a tile whose sum is cut into slices
 struct GemmW8HostArgs {
     int count;
     const int8_t *const *W;
