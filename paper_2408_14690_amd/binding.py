@@ -1115,26 +1115,43 @@ def _pitch_need(m):
     return (m + 127) // 128 * 128
 
 
-def _of_bytes(a, size, what, kind):
-    """Refuses a tensor whose values have another size than the call takes them to have."""
-    if getattr(a, "element_size", None) is not None and a.element_size() != size:
-        raise ValueError(f"{what}: {kind}")
-    return a
+def _typed(a, size, count, what, kind):
+    """_ptr of `count` values of `size` bytes each; a tensor of values of another size is refused."""
+    if a is None or isinstance(a, int):
+        return a
+    try:
+        if a.itemsize != size:
+            raise ValueError(f"{what}: {kind}")
+        if not a.is_contiguous():
+            raise ValueError("tensor arguments must be contiguous")
+        if a.nbytes < size * count:
+            raise ValueError(f"{what}: tensor of {a.nbytes} bytes, the call reads or writes {int(size * count)}")
+        return a.data_ptr()
+    except AttributeError:
+        raise TypeError(f"cannot pass {type(a).__name__} as a device pointer") from None
 
 
 def _row_floats(a, count, what):
-    return _ptr(_of_bytes(a, 4, what, "32-bit floats"), 4 * count, what)
+    return _typed(a, 4, count, what, "32-bit floats")
+
+
+_dtype_names = {}
+
+
+def _dtype_name(a):
+    dtype = getattr(a, "dtype", None)
+    if dtype not in _dtype_names:
+        _dtype_names[dtype] = str(dtype)
+    return _dtype_names[dtype]
 
 
 def teal_quantize_rows(X, type, rows, m, t, Q, row_scale, stream=None) -> int:
     """type: TEAL_F16 or TEAL_BF16; a torch tensor has to be of it."""
-    dtype = str(getattr(X, "dtype", ""))
-    if dtype.startswith("torch.") and dtype in ("torch.float16", "torch.bfloat16") and \
-            (dtype == "torch.bfloat16") != (int(type) == TEAL_BF16):
-        raise ValueError(f"X: a tensor of {dtype}, and type says another")
+    if _dtype_name(X) == ("torch.float16" if type == TEAL_BF16 else "torch.bfloat16"):
+        raise ValueError(f"X: a tensor of {X.dtype}, and type says another")
     return _call(
         "teal_quantize_rows",
-        _ptr(_of_bytes(X, 2, "X", "16-bit floats"), 2 * rows * m, "X"), int(type), int(rows), int(m), float(t),
+        _typed(X, 2, rows * m, "X", "16-bit floats"), int(type), int(rows), int(m), float(t),
         _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
 
 
@@ -1177,22 +1194,21 @@ def teal_workspace_bytes_arrange_experts(experts: int, pairs: int) -> int:
 
 
 def _numbers(a, count, what):
-    return _ptr(_of_bytes(a, 4, what, "32-bit integers"), 4 * count, what)
+    return _typed(a, 4, count, what, "32-bit integers")
 
 
 def teal_arrange_experts(idx, tokens, top_k, experts, order, start, workspace, workspace_bytes=None, stream=None) -> int:
     pairs = tokens * top_k
     return _call(
         "teal_arrange_experts",
-        _expert_numbers(idx, pairs), int(tokens), int(top_k), int(experts), _numbers(order, pairs, "order"),
+        _numbers(idx, pairs, "idx"), int(tokens), int(top_k), int(experts), _numbers(order, pairs, "order"),
         _numbers(start, experts + 1, "start"), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
 def _bf16_rows(a, count, what):
-    dtype = str(getattr(a, "dtype", ""))
-    if dtype == "torch.float16":
+    if _dtype_name(a) == "torch.float16":
         raise ValueError(f"{what}: bf16 numbers")
-    return _ptr(_of_bytes(a, 2, what, "bf16 numbers"), 2 * count, what)
+    return _typed(a, 2, count, what, "bf16 numbers")
 
 
 def teal_grouped_experts_bf16_gate_up(Wt_gate, Wt_up, experts, order, start, tokens, top_k, X_bf16, H_bf16, m, f,
@@ -1227,7 +1243,7 @@ def teal_grouped_experts_bf16_down(Wt_down, experts, order, start, tokens, top_k
     return _call(
         "teal_grouped_experts_bf16_down",
         _ptr(Wt_down, 2 * experts * m * n, "Wt_down"), int(experts), _numbers(order, pairs, "order"),
-        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _expert_numbers(idx, pairs),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _numbers(idx, pairs, "idx"),
         _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"), _row_floats(y, tokens * n, "y"),
         int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
@@ -1239,6 +1255,6 @@ def teal_grouped_experts_mx4_down(Wq_down, scale_down, experts, order, start, to
         "teal_grouped_experts_mx4_down",
         _ptr(Wq_down, experts * (m * n // 2), "Wq_down"), _ptr(scale_down, experts * _mx4_scale_need(m, n), "scale_down"),
         int(experts), _numbers(order, pairs, "order"), _numbers(start, experts + 1, "start"), int(tokens), int(top_k),
-        _expert_numbers(idx, pairs), _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"),
+        _numbers(idx, pairs, "idx"), _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"),
         _row_floats(y, tokens * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream))

@@ -44,14 +44,30 @@ __device__ __forceinline__ unsigned long long lanes_alike(int key, int bits, uns
     return same;
 }
 
+// 64 pairs a step, kSteps steps of a wavefront's pairs [begin, end) at a time: their keys, `experts` past the end.
+constexpr int kSteps = 4;
+__device__ __forceinline__ void load_keys(const ArrangeArgs &a, int begin, int end, int (&key)[kSteps])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) key[s] = key_of(a, max(min(begin + 64 * s + lane, end - 1), 0));
+}
+
 __global__ __launch_bounds__(kArrangeThreads) void count_experts_kernel(ArrangeArgs a)
 {
     __shared__ int counted[kMaxExperts + 1];
     const int keys = a.experts + 1;
     for (int e = threadIdx.x; e < keys; e += kArrangeThreads) counted[e] = 0;
     __syncthreads();
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int begin = blockIdx.x * a.chunk, end = min(a.pairs, begin + a.chunk);
-    for (int p = begin + (int)threadIdx.x; p < end; p += kArrangeThreads) atomicAdd(&counted[key_of(a, p)], 1);
+    for (int p = begin + w * 64 * kSteps; p < end; p += kArrangeThreads * kSteps) {
+        int key[kSteps];
+        load_keys(a, p, end, key);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            if (p + 64 * s + lane < end) atomicAdd(&counted[key[s]], 1);
+    }
     __syncthreads();
     for (int e = threadIdx.x; e < keys; e += kArrangeThreads) a.counts[blockIdx.x * keys + e] = counted[e];
 }
@@ -66,21 +82,17 @@ __global__ __launch_bounds__(kArrangeThreads) void place_pairs_kernel(ArrangeArg
     const int keys = a.experts + 1;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int begin = blockIdx.x * a.chunk, end = min(a.pairs, begin + a.chunk);
-    const int share = (a.chunk + kArrangeThreads - 1) / kArrangeThreads * 64;
+    const int share = a.chunk / kArrangeThreads * 64;
     const int p0 = begin + w * share, p1 = min(end, p0 + share);
-    for (int e = lane; e < keys; e += 64) at[w][e] = 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int p = p0 + lane; p < p1; p += 64) atomicAdd(&at[w][key_of(a, p)], 1);
-    __syncthreads();
+    int key[kSteps];
+    if (p0 < p1) load_keys(a, p0, p1, key);
 
-    // Thread e has expert e (and the threads at the end of the block those from kArrangeThreads on: one at most).
+    // Thread e has expert e (and the last one the key of no expert, where there are as many experts as threads).
     static_assert(kMaxExperts == kArrangeThreads, "an expert a thread, and one more key");
     int total = 0, before = 0;           // of all chunks, of the chunks before this one
     const int e = threadIdx.x;
-    if (e < keys) {
-        if constexpr (ALONE) {
-            for (int v = 0; v < kArrangeWaves; ++v) total += at[v][e];
-        } else {
+    if constexpr (!ALONE) {
+        if (e < keys) {
             // several on their way together: one after the other each would take a trip to memory
             const int chunks = gridDim.x;
             for (int c0 = 0; c0 < chunks; c0 += 32) {
@@ -95,6 +107,17 @@ __global__ __launch_bounds__(kArrangeThreads) void place_pairs_kernel(ArrangeArg
             }
         }
     }
+    for (int k = lane; k < keys; k += 64) at[w][k] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int p = p0; p < p1; p += 64 * kSteps) {
+        if (p > p0) load_keys(a, p, p1, key);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            if (p + 64 * s + lane < p1) atomicAdd(&at[w][key[s]], 1);
+    }
+    __syncthreads();
+    if (ALONE && e < keys)
+        for (int v = 0; v < kArrangeWaves; ++v) total += at[v][e];
     const int upto = wave_inclusive_scan(total);
     if (lane == 63) sums[w] = upto;
     __syncthreads();
@@ -125,18 +148,22 @@ __global__ __launch_bounds__(kArrangeThreads) void place_pairs_kernel(ArrangeArg
     __syncthreads();
 
     const int bits = 32 - __builtin_clz(a.experts);
-    for (int p = p0; p < p1; p += 64) {                            // wavefront-uniform
-        const bool live = p + lane < p1;
-        const int key = live ? key_of(a, p + lane) : 0;
-        const unsigned long long same = lanes_alike(key, bits, __ballot(live));
-        const int rank = lanes_below(same);
-        if (live) {
-            const int place = at[w][key] + rank;
-            if (place < a.pairs) a.order[place] = p + lane;        // (idx may not change meanwhile; if it does, nothing breaks)
+    for (int p = p0; p < p1; p += 64 * kSteps) {                   // wavefront-uniform
+        if (share > 64 * kSteps) load_keys(a, p, p1, key);         // (else they are still there)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const bool live = p + 64 * s + lane < p1;
+            const unsigned long long same = lanes_alike(key[s], bits, __ballot(live));
+            const int rank = lanes_below(same);
+            if (live) {
+                const int place = at[w][key[s]] + rank;
+                // (idx may not change meanwhile; if it does, nothing outside `order` is written)
+                if ((unsigned)place < (unsigned)a.pairs) a.order[place] = p + 64 * s + lane;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (live && rank == 0) at[w][key[s]] += __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (live && rank == 0) at[w][key] += __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
