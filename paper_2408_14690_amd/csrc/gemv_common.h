@@ -338,13 +338,13 @@ struct HalfSource {                   // the hidden state itself, fp16 in memory
     __device__ __forceinline__ float value(Raw r, float) const { return (float)r; }
 };
 
-// SiLU(g) * u (Appendix A.3: the input of W_down) in stated binary32 arithmetic,
-// because its rounding to fp16 decides the mask: clamp -g to
+// SiLU(g) * u rounded to fp16 (Appendix A.3: the input of W_down), in stated
+// binary32 arithmetic, because this value decides the mask: clamp -g to
 // [-80, 80]; exp by k = rint(z log2 e), r = z - k ln2 (two fmas, ln2 split
 // high / low), the degree-7 Taylor polynomial by Horner's rule with fmas, exact
 // scaling by 2^k; sigma = 1 / (1 + e) (correctly rounded division);
-// SiLU = g * sigma; times u.  NaN in, NaN out.
-__device__ __forceinline__ float swiglu_product(float g, float u)
+// SiLU = g * sigma; times u; round to nearest even.  NaN in, NaN out.
+__device__ __forceinline__ float swiglu_value(float g, float u)
 {
 #pragma clang fp contract(off)
     const float z = __builtin_amdgcn_fmed3f(-g, -80.0f, 80.0f);      // (of a NaN: any number, see below)
@@ -362,13 +362,7 @@ __device__ __forceinline__ float swiglu_product(float g, float u)
     const float e = ldexpf(p, (int)k);
     const float sg = 1.0f / (1.0f + e);
     const float silu = g != g ? g : g * sg;
-    return silu * u;
-}
-
-// Rounded to fp16, to nearest even.
-__device__ __forceinline__ float swiglu_value(float g, float u)
-{
-    float h32 = swiglu_product(g, u);
+    float h32 = silu * u;
     // The product is rounded to binary32 first and to binary16 second.  Without this
     // fence the compiler folds the two into one mixed-precision instruction that rounds
     // the exact product once, which differs from the stated arithmetic near ties.

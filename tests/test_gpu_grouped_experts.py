@@ -3,12 +3,13 @@
 Tolerances.  A product of two bf16 numbers has 16 significant bits: exact in fp32.  A sum of m of them in fp32, in any order,
 is off by at most m * 2^-23 * sum |x w| (an addition by half a step of its result, 2^-24; the matrix cores may cut where
 they do not round, 2^-23).  Weights and joins of top_k rows add top_k + 1 roundings of 2^-24.  For H the products'
-errors go through SiLU(g) * u, whose derivatives are at most 1.1 |u| and |g| in size, the stated arithmetic is off by at most 2^-20
-of its value, and the rounding to bf16 by 2^-8 of it.  Where everything is a small whole number nothing is off at all."""
+errors go through SiLU(g) * u, whose derivatives are at most 1.1 |u| and |g| in size, SiLU(g) * u itself is off by less than
+2^-16 of its value, as the header says, and the rounding to bf16 by 2^-8 of it.  Where everything is a small whole number the sums
+are not off at all."""
 import numpy as np
 import pytest
 
-from test_gpu_many_rows import FILL, swiglu_f32
+from test_gpu_many_rows import FILL
 from test_gpu_mx4 import T  # noqa: F401
 
 torch = pytest.importorskip("torch")
@@ -149,7 +150,7 @@ class Case:
             g, u = x @ self.gate64[e], x @ self.up64[e]
             off_g, off_u = (self.m * 2.0 ** -23 * (x.abs() @ w[e].abs()) for w in (self.gate64, self.up64))
             want = g * torch.sigmoid(g) * u
-            off = 1.1 * off_g * (u.abs() + off_u) + off_u * g.abs() + want.abs() * (2.0 ** -8 + 2.0 ** -20) + 2.0 ** -133
+            off = 1.1 * off_g * (u.abs() + off_u) + off_u * g.abs() + want.abs() * (2.0 ** -8 + 2.0 ** -16) + 2.0 ** -133
             assert bool(((h[at].double() - want).abs() <= off).all()), e
         return h
 
@@ -188,15 +189,19 @@ def test_bf16_widths_in_steps_of_eight(T, tokens, top_k, experts, m, f, n):   # 
 @pytest.mark.parametrize("fmt", ["bf16", "mx4"])
 @pytest.mark.parametrize("tokens,top_k,experts,m,f,n", [(9, 2, 8, 72, 64, 96), (200, 2, 4, 136, 96, 320), (900, 2, 2, 264, 160, 544)])
 def test_whole_numbers_come_out_exactly(T, fmt, tokens, top_k, experts, m, f, n):   # noqa: F811
-    """Products and sums of small whole numbers, and weights that are powers of two: every bit is determined, of H by the
-    stated arithmetic."""
+    """Products and sums of small whole numbers, and weights that are powers of two: every bit of y is determined, and H lies
+    between the roundings of what is 2^-16 smaller and larger."""
     c = Case(T, fmt, tokens, top_k, experts, m, f, n, whole=True)
     h = c.run_gate_up()
     for e, at, pairs in c.places():
         x = c.x[pairs // top_k].double()
-        g, u = ((x @ w[e]).float().cpu().numpy() for w in (c.gate64, c.up64))
-        want = torch.from_numpy(swiglu_f32(g, u)).bfloat16()
-        assert torch.equal(h[at].cpu(), want), e
+        g, u = x @ c.gate64[e], x @ c.up64[e]
+        want = g * torch.sigmoid(g) * u
+        ends = torch.stack([(want * (1 + s)).float().bfloat16() for s in (-2.0 ** -16, 2.0 ** -16)])
+        ok = (h[at] >= ends.amin(0)) & (h[at] <= ends.amax(0))
+        # |SiLU(g)| <= 87 e^-87 < 1.5e-36 for g <= -87; where 1 / (1 + e^-g) is below 2^-126 = e^-87.3 it may count as zero
+        ok |= (g < -87) & (h[at].double().abs() <= 1.5e-36 * u.abs())
+        assert bool(ok.all()), e
     h = torch.randint(-3, 4, (c.pairs, f), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
     y = c.run_down(h)
     want = torch.zeros(c.pairs, n, dtype=torch.float64, device="cuda")
