@@ -590,6 +590,12 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
  *   workspace  at least teal_workspace_bytes_gemm_w8(rows, m, n_0 + ... + n_{count-1}) bytes, zero before first use
  *           like every workspace.  No survivor counts.
  *   TEAL_ERR_SHAPE also where rows and widths make more blocks than one launch has (2^22 tiles of 32 x 128).
+ * teal_gemm_w8_ex: teal_gemm_w8_multi with the launch shape chosen by the caller, for tuning and for tests that walk the
+ * kernel variants; the results are the same, bit for bit.  0 means the library's choice (of all three, or of splits: 1).
+ *   tile_rows, tile_cols  rows and columns of a block's tile: 16, 32, 64, 128 or 256 by 128, or 256 by 256.
+ *   splits  1..16: blocks along the sum, more than one with at most 128 rows and 512 blocks; a request of more than
+ *           there are slabs of 128 channels runs with fewer.
+ *   Else TEAL_ERR_UNSUPPORTED.  workspace: with splits of at least teal_workspace_bytes_gemm_w8(tile_rows, m, n).
  */
 #define TEAL_F16 0
 #define TEAL_BF16 1
@@ -606,6 +612,9 @@ teal_status teal_gemm_w8(const int8_t *Wq, const void *scale_f16, const int8_t *
 teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
                                const int *n, const int8_t *Q, const float *row_scale, int rows, int m,
                                void *workspace, size_t workspace_bytes, void *stream);
+teal_status teal_gemm_w8_ex(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
+                            const int *n, const int8_t *Q, const float *row_scale, int rows, int m, void *workspace,
+                            size_t workspace_bytes, void *stream, int tile_rows, int tile_cols, int splits);
 
 /*
  * A mixture of experts for many tokens: the pairs (token, expert) that teal_route_experts chose, sorted by expert, and

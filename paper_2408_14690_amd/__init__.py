@@ -33,7 +33,7 @@ from .binding import (  # noqa: F401
     teal_sparse_experts_bf16_swiglu, teal_sparse_experts_mx4_swiglu,
     TEAL_F16, TEAL_BF16, TEAL_MAX_ROWS, TEAL_MAX_ROW_SUM,
     teal_quantized_pitch, teal_quantize_rows, teal_quantize_rows_swiglu, teal_workspace_bytes_gemm_w8,
-    teal_gemm_w8, teal_gemm_w8_multi, teal_workspace_bytes_arrange_experts, teal_arrange_experts,
+    teal_gemm_w8, teal_gemm_w8_multi, teal_gemm_w8_ex, teal_workspace_bytes_arrange_experts, teal_arrange_experts,
     teal_grouped_experts_bf16_gate_up, teal_grouped_experts_mx4_gate_up, teal_workspace_bytes_grouped_experts,
     teal_grouped_experts_bf16_down, teal_grouped_experts_mx4_down,
 )

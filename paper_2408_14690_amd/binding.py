@@ -49,7 +49,7 @@ EXPORTS = (
     "teal_route_experts", "teal_workspace_bytes_experts", "teal_sparse_experts_bf16",
     "teal_sparse_experts_mx4", "teal_sparse_experts_bf16_swiglu", "teal_sparse_experts_mx4_swiglu",
     "teal_quantized_pitch", "teal_quantize_rows", "teal_quantize_rows_swiglu", "teal_workspace_bytes_gemm_w8",
-    "teal_gemm_w8", "teal_gemm_w8_multi", "teal_workspace_bytes_arrange_experts", "teal_arrange_experts",
+    "teal_gemm_w8", "teal_gemm_w8_multi", "teal_gemm_w8_ex", "teal_workspace_bytes_arrange_experts", "teal_arrange_experts",
     "teal_grouped_experts_bf16_gate_up", "teal_grouped_experts_mx4_gate_up", "teal_workspace_bytes_grouped_experts",
     "teal_grouped_experts_bf16_down", "teal_grouped_experts_mx4_down",
 )
@@ -255,6 +255,8 @@ def load_library():
     lib.teal_gemm_w8.argtypes = [vp, vp, vp, vp, i, vp, i, i, vp, sz, vp]
     lib.teal_gemm_w8_multi.restype = i
     lib.teal_gemm_w8_multi.argtypes = [i, vp, vp, vp, vp, vp, vp, i, i, vp, sz, vp]
+    lib.teal_gemm_w8_ex.restype = i
+    lib.teal_gemm_w8_ex.argtypes = [i, vp, vp, vp, vp, vp, vp, i, i, vp, sz, vp, i, i, i]
     lib.teal_workspace_bytes_arrange_experts.restype = sz
     lib.teal_workspace_bytes_arrange_experts.argtypes = [i, i]
     lib.teal_arrange_experts.restype = i
@@ -1174,19 +1176,30 @@ def teal_gemm_w8(Wq, scale_f16, Q, row_scale, rows, Y, m, n, workspace, workspac
         _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
-def teal_gemm_w8_multi(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m, workspace, workspace_bytes=None,
-                       stream=None) -> int:
-    """len(Wq_list) matrices on the same rows; the per-matrix lists become host arrays."""
+def _gemm_w8_arguments(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m, workspace, workspace_bytes, stream):
     count = len(Wq_list)
     if not (len(scale_list) == len(Y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
     W = _pointers([_ptr(w, m * n, "Wq") or 0 for w, n in zip(Wq_list, n_list)])
     S = _pointers([_ptr(sc, 2 * n, "scale") or 0 for sc, n in zip(scale_list, n_list)])
     Y = _pointers([_row_floats(y, rows * n, "Y") or 0 for y, n in zip(Y_list, n_list)])
-    return _call(
-        "teal_gemm_w8_multi",
-        count, W, S, Y, _ints(n_list), _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"),
-        int(rows), int(m), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+    return (count, W, S, Y, _ints(n_list), _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"),
+            int(rows), int(m), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+
+
+def teal_gemm_w8_multi(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m, workspace, workspace_bytes=None,
+                       stream=None) -> int:
+    """len(Wq_list) matrices on the same rows; the per-matrix lists become host arrays."""
+    return _call("teal_gemm_w8_multi", *_gemm_w8_arguments(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m,
+                                                           workspace, workspace_bytes, stream))
+
+
+def teal_gemm_w8_ex(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m, workspace, workspace_bytes=None,
+                    stream=None, tile_rows=0, tile_cols=0, splits=0) -> int:
+    """teal_gemm_w8_multi with a launch shape of the caller's choice."""
+    return _call("teal_gemm_w8_ex", *_gemm_w8_arguments(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, m,
+                                                        workspace, workspace_bytes, stream),
+                 int(tile_rows), int(tile_cols), int(splits))
 
 
 def teal_workspace_bytes_arrange_experts(experts: int, pairs: int) -> int:

@@ -1517,8 +1517,8 @@ teal_status teal_quantize_rows_swiglu(const float *gate, const float *up, int ro
 // takes a compute unit `alone` microseconds with one block on it, `pair` with two (0: LDS has no room for two), measured on
 // full launches (4096 x 8192 -> 28672 rows in 256 x 256 tiles 7 x 64 slabs in 840 us, 2048 x 14336 -> 4096 in 256 x 128 112
 // in 120; 333 x 5001 -> 3840 in 128 x 128 20 in 14 beside what the launch's ends take, in 64 x 128 40 in 17).  Weights come
-// from memory at 4.6 TB/s and all that the tiles load from the caches at 12.  Slices take 2 us more and their sums' way to memory and back at 4.5 TB/s, to the
-// one block that adds a tile's at 0.1.
+// from memory at 4.6 TB/s and all that the tiles load from the caches at 12.  Slices take 2 us more and their sums' way to
+// memory and back at 4.5 TB/s, to the one block that adds a tile's at 0.1.
 struct GemmTiles {
     int bm, bn;
     double alone, pair;
@@ -1571,9 +1571,9 @@ size_t teal_workspace_bytes_gemm_w8(int rows, int m, int n)
     return teal::kCounterBytes + (size_t)kMaxSlicedBlocks * bm * 128 * sizeof(int);
 }
 
-teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
-                               const int *n, const int8_t *Q, const float *row_scale, int rows, int m, void *workspace,
-                               size_t workspace_bytes, void *stream)
+teal_status teal_gemm_w8_ex(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
+                            const int *n, const int8_t *Q, const float *row_scale, int rows, int m, void *workspace,
+                            size_t workspace_bytes, void *stream, int tile_rows, int tile_cols, int splits)
 {
     if (count < 1 || count > teal::kMaxMatrices) return TEAL_ERR_UNSUPPORTED;
     if (!Wq || !scale_f16 || !Y || !n || !workspace) return TEAL_ERR_NULL;
@@ -1594,7 +1594,31 @@ teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *c
     if (rows == 0) return TEAL_OK;
     const teal::GemmW8HostArgs h{count, Wq, scale_f16, Y, n, Q, row_scale, rows, m, ws_counters(workspace),
                                  ws_counters(workspace) + teal::kCounterBytes / sizeof(int)};
-    return from_hip(teal::launch_gemm_w8(h, gemm_w8_shape(rows, m, n, count), static_cast<hipStream_t>(stream)));
+    teal::GemmShape shape;
+    if (tile_rows == 0 && tile_cols == 0 && splits == 0) {
+        shape = gemm_w8_shape(rows, m, n, count);
+    } else {
+        shape = {tile_rows, tile_cols, splits == 0 ? 1 : splits};
+        bool known = false;
+        long long blocks = 0;
+        for (const GemmTiles &t : kGemmTiles) known = known || (t.bm == tile_rows && t.bn == tile_cols);
+        if (!known || shape.splits < 1 || shape.splits > 16) return TEAL_ERR_UNSUPPORTED;
+        for (int k = 0; k < count; ++k) blocks += (n[k] + shape.bn - 1) / shape.bn;
+        blocks *= (long long)((rows + shape.bm - 1) / shape.bm) * shape.splits;
+        if (blocks > kMaxTiles) return TEAL_ERR_UNSUPPORTED;
+        if (shape.splits > 1) {
+            if (shape.bm > teal::kMaxSlicedRows || blocks > kMaxSlicedBlocks) return TEAL_ERR_UNSUPPORTED;
+            if (workspace_bytes < teal_workspace_bytes_gemm_w8(shape.bm, m, (int)n_total)) return TEAL_ERR_WORKSPACE;
+        }
+    }
+    return from_hip(teal::launch_gemm_w8(h, shape, static_cast<hipStream_t>(stream)));
+}
+
+teal_status teal_gemm_w8_multi(int count, const int8_t *const *Wq, const void *const *scale_f16, float *const *Y,
+                               const int *n, const int8_t *Q, const float *row_scale, int rows, int m, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    return teal_gemm_w8_ex(count, Wq, scale_f16, Y, n, Q, row_scale, rows, m, workspace, workspace_bytes, stream, 0, 0, 0);
 }
 
 teal_status teal_gemm_w8(const int8_t *Wq, const void *scale_f16, const int8_t *Q, const float *row_scale, int rows,

@@ -181,6 +181,17 @@ def test_grouped_experts(T, fmt, tokens, top_k, experts, m, f, n):   # noqa: F81
     Case(T, fmt, tokens, top_k, experts, m, f, n, padded=tokens // 7).check()
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("f,n", [(1024, 2048), (2048, 4096), (96, 160)])
+def test_large_groups_whose_last_tiles_are_more_or_less_empty(T, fmt, f, n):   # noqa: F811
+    """The shapes that many rows take (128 or 256 rows by 128 or 256 columns), and last tiles of few rows, about a quarter, half,
+    three quarters and all of them."""
+    sizes = [512 + 20, 3 * 256 + 64, 256 + 65, 2 * 256 + 128, 256 + 129, 256 + 192, 256 + 193, 1024, 7, 0]
+    choose = np.repeat(np.arange(len(sizes), dtype=np.int32), sizes)
+    choose = np.random.default_rng(f).permutation(choose)[:, None]
+    Case(T, fmt, choose.shape[0], 1, len(sizes), 136, f, n, choose=choose).check()
+
+
 @pytest.mark.parametrize("tokens,top_k,experts,m,f,n", [(3, 2, 4, 8, 8, 8), (50, 3, 5, 40, 24, 72), (300, 2, 2, 24, 136, 264)])
 def test_bf16_widths_in_steps_of_eight(T, tokens, top_k, experts, m, f, n):   # noqa: F811
     Case(T, "bf16", tokens, top_k, experts, m, f, n).check()

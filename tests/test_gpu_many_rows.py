@@ -185,9 +185,35 @@ def test_products_with_a_sum_cut_into_slices(T, rows, m, widths):   # noqa: F811
     check_products(T, rows, m, widths)
 
 
-@pytest.mark.parametrize("rows,m,widths", [(1024, 384, [12288]), (2050, 200, [8192 + 16, 48]), (4096, 130, [4096])])
+@pytest.mark.parametrize("rows,m,widths", [(1024, 384, [12288]), (2050, 200, [8192 + 16, 48]), (4096, 130, [4096]),
+                                           (700, 11008, [4096]), (1000, 2048, [8192])])
 def test_products_of_large_tiles(T, rows, m, widths):   # noqa: F811
     check_products(T, rows, m, widths)
+
+
+@pytest.mark.parametrize("tile_rows,tile_cols", [(16, 128), (32, 128), (64, 128), (128, 128), (256, 128), (256, 256)])
+def test_every_launch_shape(T, tile_rows, tile_cols):   # noqa: F811
+    """All tiles, with last ones of a quarter, half and three quarters of their rows, whole and cut sums, ragged columns and
+    channels: the same bits."""
+    gen = torch.Generator(device="cuda").manual_seed(tile_rows + tile_cols)
+    for rows, m, widths in [(1, 300, [144]), (tile_rows, 129, [256, 48]), (tile_rows // 4, 640, [272]), (tile_rows // 2 + 1, 1000, [528]),
+                            (tile_rows * 2 + tile_rows * 3 // 4, 257, [400]), (tile_rows * 3 + tile_rows // 2, 1300, [112, 16, 336]),
+                            (tile_rows + tile_rows // 4, 100, [512]), (9 * tile_rows + 7, 384, [1040])]:
+        q, row_scale = make_rows(T, gen, rows, m)
+        W = [random_ints(gen, m, n, low=-128) for n in widths]
+        scale = [(torch.rand(n, generator=gen, device="cuda") * 0.01 + 1e-3).half() for n in widths]
+        ws = torch.zeros(T.teal_workspace_bytes_gemm_w8(max(rows, tile_rows), m, sum(widths)), dtype=torch.uint8, device="cuda")
+        blocks = -(-rows // tile_rows) * sum(-(-n // tile_cols) for n in widths)
+        for splits in (1, 2, 3, 8, 16):
+            if splits > 1 and (tile_rows > 128 or blocks * splits > 512):
+                continue
+            ys = [torch.full((rows + 1, n), FILL, device="cuda") for n in widths]
+            T.check(T.teal_gemm_w8_ex(W, scale, ys, widths, q, row_scale, rows, m, ws, tile_rows=tile_rows, tile_cols=tile_cols,
+                                      splits=splits))
+            for y, w, s in zip(ys, W, scale):
+                assert bool((y[rows] == FILL).all())
+                assert torch.equal(y[:rows], product(q, row_scale, w, s)), (rows, m, widths, splits)
+            assert bool((ws[:1 << 20] == 0).all())
 
 
 def test_one_workspace_for_calls_of_all_sizes(T):   # noqa: F811

@@ -68,6 +68,22 @@ def test_gemm_w8_refusals(multi):
         assert T.teal_workspace_bytes_gemm_w8(a["rows"], a["m"], a["n"]) == 0, kw
 
 
+def test_gemm_w8_ex_refuses_shapes_that_there_are_not():
+    def run(tile_rows, tile_cols, splits, rows=5, n=64, wb=BIG):
+        return T.teal_gemm_w8_ex([W], [SC], [Y], [n], X, G, rows, 4096, WS, wb, stream=0, tile_rows=tile_rows,
+                                 tile_cols=tile_cols, splits=splits)
+
+    for shape in [(8, 128, 1), (16, 256, 1), (128, 256, 1), (64, 64, 1), (0, 128, 1), (64, 0, 1), (0, 0, 2), (512, 128, 1), (64, 128, -1),
+                  (64, 128, 17), (256, 128, 2), (256, 256, 2), (-16, 128, 1)]:
+        assert run(*shape) == T.TEAL_ERR_UNSUPPORTED, shape
+    assert run(16, 128, 2, rows=16 * 300) == T.TEAL_ERR_UNSUPPORTED                # more blocks than sliced sums have room for
+    # 2^16 tiles of 16 rows by 128 of 128 columns are 2^23 blocks, more than the 2^22 of a launch; of 32 rows they would fit.
+    assert run(16, 128, 1, rows=1 << 20, n=16384) == T.TEAL_ERR_UNSUPPORTED
+    small = T.teal_workspace_bytes_gemm_w8(5, 4096, 64)
+    assert small < T.teal_workspace_bytes_gemm_w8(128, 4096, 64)
+    assert run(128, 128, 2, wb=small) == T.TEAL_ERR_WORKSPACE
+
+
 def test_arrange_refusals():
     ok = dict(idx=I, tokens=5, top_k=2, experts=8, order=X, start=Y, ws=WS, wb=BIG)
 
