@@ -566,6 +566,10 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
  * is a hidden state of its own.  Dense but for the threshold of teal_quantize_rows: what many rows keep together is
  * every channel, so nothing is left to skip (Section 5.4.3 discusses a prompt's first half for its accuracy).
  *
+ * The calls of this part and the next leave sums and counts in their workspaces.  One may serve them and the calls whose
+ * workspace is teal_workspace_bytes or those of a batch or of experts in turn; a workspace of groups (_stack) or of a
+ * whole MLP, whose counters lie further on, keeps to its own calls.
+ *
  * 8-bit weights (Section 5.3), W[j][i] = Wq[i][j] * scale[j] as for teal_sparse_gemv_w8: rows to 8-bit integers with a
  * scale each, and products of integers.
  *

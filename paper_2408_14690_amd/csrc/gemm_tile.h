@@ -2,18 +2,25 @@
 // input-channel-major as the one-row products store it (Wt[m][n], n contiguous).
 //
 // A block takes BM rows by BN columns and walks the sum in slabs of 128 bytes of a row of X: 64 channels of bf16, 128 of
-// int8.  X and W travel from memory into LDS without registers (global_load_lds), in a ring of STAGES slabs: one
-// barrier a slab, the loads of the slab STAGES - 1 further in flight while a slab is multiplied.  The matrix
-// instructions (16 x 16, K = 32 for bf16, 64 for int8) want both operands contiguous along the sum in a lane; X is, and W comes
-// through the transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block of 16-bit values and get a
-// column each; ds_read_b64_tr_b8: an 8 x 16 block of bytes).  W is the first operand and X the second, so a lane ends
-// up with four neighbouring columns of one row, 16 bytes of y.
+// int8.  X and W travel from memory into LDS without registers (global_load_lds), in a ring of STAGES slabs: one barrier a
+// slab, the loads of the slab STAGES - 1 further in flight while a slab is multiplied.  The matrix instructions (16 x 16,
+// K = 32 for bf16, 64 for int8) want both operands contiguous along the sum in a lane; X is, and W comes through the
+// transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block of 16-bit values and get a column each;
+// ds_read_b64_tr_b8: an 8 x 16 block of bytes).  W is the first operand and X the second, so a lane ends up with four
+// neighbouring columns of one row, 16 bytes of y.
 //
-// LDS banks.  A row of X in LDS is 128 bytes, 8 chunks of 16: chunk c of row r is at place c ^ (r & 7), so 8 lanes
-// that read one chunk of 8 rows touch all banks.  A row of W has 32-byte units (bf16) or 16-byte units (int8), what one
-// row gives to a transposing read: unit u of channel k is at place u ^ swizzle(k), so that the 4 (8) rows of a group of
-// 16 lanes, and the groups of two halves of a wavefront, touch different banks.  The direct loads fill LDS linearly; the
+// LDS banks.  A row of X in LDS is 128 bytes, 8 chunks of 16: chunk c of row r is at place c ^ (r & 7), so 8 lanes that
+// read one chunk of 8 rows touch all banks.  A row of W has 32-byte units (bf16) or 16-byte units (int8), what one row
+// gives to a transposing read: unit u of channel k is at place u ^ swizzle(k), so that the 4 (8) rows of a group of 16
+// lanes, and the groups of two halves of a wavefront, touch different banks.  The direct loads fill LDS linearly; the
 // permutation is in the lanes' global addresses, within one row's bytes.
+//
+// What bounds it.  Tiles up to 256 x 128: the way from the L2 caches into LDS, which gives all compute units together about
+// 12 TB/s whatever the tile (int8, 700 rows of 11008 -> 4096: 46 us; with every wavefront loading its part 55, since the
+// address arithmetic and the waits of the loads then stand between its matrix instructions).  256 x 256 loads least for what
+// it multiplies (9 TB/s) and has the matrix cores busy; there their rate, which falls with the power that the operands'
+// bits take (7 to 20 % between zeros and random numbers), bounds it with the LDS reads: 4096 x 8192 -> 28672 int8 at
+// 2.26 POPS.  Tiles of few rows: memory, once for W.
 #pragma once
 
 #include "gemv_common.h"
@@ -104,7 +111,6 @@ struct TileProduct {
     static constexpr int kRowStep = kRowsPerLoad * kLoadWaves;
     static constexpr int kUnit = F::kBytes == 2 ? 32 : 16;             // bytes that a permutation keeps together
     static constexpr int kUnitMask = kRowBytes / HALVES / kUnit < 16 ? kRowBytes / HALVES / kUnit - 1 : 15;
-    static constexpr int kHalfCols = BN / HALVES;
     // A lane's permutation in its loads of W repeats with the bits of the row that it depends on.
     static constexpr int kPeriod = F::kBytes == 2 ? 16 : 32;
     static constexpr int kWLanes = F::kMx4 || kRowStep % kPeriod == 0 ? 1 : 2;
@@ -303,7 +309,8 @@ struct TileProduct {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
                     typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
                     const int k = 32 * ks + 8 * g + l / 4;             // and 4 further
-                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 + l % 4 * 8;      // flip(k) is 0
+                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 +
+                                      l % 4 * 8;                       // flip(k) is 0
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
                     const lds_ptr p4 = w + (k + 4) * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 +
                                        (l % 4 * 8 ^ flip(4));
@@ -360,7 +367,7 @@ struct TileProduct {
         if constexpr (F::kMx4) {
             if (loads) load_w(first, STAGES - 1, m);
             wait_and_meet<0>();
-            if (multiplies()) convert(read_block(STAGES - 1), first, 0, m);      // (the place is filled after the next meeting)
+            if (multiplies()) convert(read_block(STAGES - 1), first, 0, m);      // (filled again after the next meeting)
         }
         // Place s of the ring: X of slab first + s, and W of the same slab (mx4: of the next one).
         if (loads) {

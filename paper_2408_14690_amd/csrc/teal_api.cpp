@@ -508,7 +508,7 @@ const char *teal_status_string(teal_status s)
     return "unknown status";
 }
 
-int teal_version(void) { return 419; }
+int teal_version(void) { return 420; }
 
 size_t teal_survivors_offset(void) { return teal::kCounterBytes; }
 
@@ -1477,7 +1477,7 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
 
 static_assert(TEAL_MAX_ROW_SUM == teal::kMaxRowSum, "the limit the header states is the kernel's");
 
-// A launch holds fewer than 2^32 threads: tiles of 32 rows by 128 columns, the smallest, have 256 each.
+// Blocks of a launch: it holds fewer than 2^32 threads, and a block has 768 at most.
 static constexpr long long kMaxTiles = 1 << 22;
 
 int teal_quantized_pitch(int m) { return m < 1 || m > TEAL_MAX_ROW_SUM ? 0 : teal::quantized_pitch(m); }

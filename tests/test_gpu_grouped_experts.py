@@ -269,6 +269,37 @@ def test_one_bad_row_stays_in_its_row(T, fmt, tokens):   # noqa: F811
     assert torch.equal(y[keep], clean_y[keep]) and bool(torch.isnan(y[5]).all())
 
 
+@pytest.mark.parametrize("fmt,n", [("bf16", 1032), ("mx4", 1056)])
+def test_sums_of_more_pairs_than_the_workspace_has_rows_of(T, fmt, n):   # noqa: F811
+    """W_down in parts of 512 columns, the last one of 8 or 32: the rows of all columns would be more than 256 MB."""
+    c = Case(T, fmt, 50000, 2, 8, 32, 32, n, padded=3)
+    assert T.teal_workspace_bytes_grouped_experts(c.pairs, n) < (1 << 20) + c.pairs * n * 4
+    c.check()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+def test_two_mixtures_at_once(T, fmt):   # noqa: F811
+    """On two streams with a workspace each."""
+    sides = []
+    for seed in (1, 2):
+        c = Case(T, fmt, 300 * seed, 2, 8, 128, 96, 256, seed=seed)
+        h = c.run_gate_up()
+        sides.append((c, h, c.run_down(h), torch.cuda.Stream(), torch.empty_like(h), torch.empty(c.tokens, c.n, device="cuda"),
+                      torch.zeros(T.teal_workspace_bytes_grouped_experts(c.pairs, c.n), dtype=torch.uint8, device="cuda")))
+    gate_up = T.teal_grouped_experts_bf16_gate_up if fmt == "bf16" else T.teal_grouped_experts_mx4_gate_up
+    down = T.teal_grouped_experts_bf16_down if fmt == "bf16" else T.teal_grouped_experts_mx4_down
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, _, _, stream, h, y, ws in sides:
+            s = stream.cuda_stream
+            T.check(T.teal_arrange_experts(c.idx, c.tokens, c.top_k, c.experts, c.order, c.start, ws, stream=s))
+            T.check(gate_up(*c.gate, *c.up, c.experts, c.order, c.start, c.tokens, c.top_k, c.x, h, c.m, c.f, stream=s))
+            T.check(down(*c.down, c.experts, c.order, c.start, c.tokens, c.top_k, c.idx, c.weight, h, y, c.f, c.n, ws, stream=s))
+    torch.cuda.synchronize()
+    for c, want_h, want, _, h, y, _ in sides:
+        assert torch.equal(h, want_h) and torch.equal(y, want)
+
+
 def test_the_weight_of_a_pair_without_an_expert_adds_nothing(T):   # noqa: F811
     c = Case(T, "bf16", 30, 3, 4, 64, 64, 64, choose=np.tile(np.array([[1, -1, 2]], np.int32), (30, 1)))
     h = c.run_gate_up()

@@ -306,3 +306,65 @@ def test_rows_of_a_batch_are_what_one_row_gives(T):   # noqa: F811
         part = torch.empty(b - a, n, device="cuda")
         T.check(T.teal_gemm_w8(W, scale, q[a:b], row_scale[a:b], b - a, part, m, n, ws))
         assert torch.equal(part, whole[a:b])
+
+
+def test_one_workspace_with_the_calls_of_one_row(T):   # noqa: F811
+    """Calls of one row, of a few and of many in turn on one workspace: each leaves it ready for the others."""
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    m, n = 4096, 1024
+    W, scale = random_ints(gen, m, n), (torch.rand(n, generator=gen, device="cuda") * 0.01).half()
+    Wt = torch.randn(m, n, generator=gen, device="cuda").bfloat16()
+    x = torch.randn(40, m, generator=gen, device="cuda").half()
+    q, row_scale = make_rows(T, gen, 40, m)
+    fresh = [torch.empty(n, device="cuda"), torch.empty(4, n, device="cuda")]
+    size = max(T.teal_workspace_bytes(m, n), T.teal_workspace_bytes_batch(4, m, n), T.teal_workspace_bytes_gemm_w8(40, m, n))
+
+    def one(y, ws):
+        T.check(T.teal_sparse_gemv_w8(W, scale, x[0], 0.5, y, m, n, ws))
+
+    def few(y, ws):
+        T.check(T.teal_sparse_gemv_bf16_batch(Wt, x[:4], 4, 0.5, y, m, n, ws))
+
+    for call, y in zip((one, few), fresh):
+        call(y, torch.zeros(size, dtype=torch.uint8, device="cuda"))
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    many = torch.empty(40, n, device="cuda")
+    for splits in (0, 4, 16):
+        T.check(T.teal_gemm_w8_ex([W], [scale], [many], [n], q, row_scale, 40, m, ws, tile_rows=64 if splits else 0,
+                                  tile_cols=128 if splits else 0, splits=splits))
+        assert torch.equal(many, product(q, row_scale, W, scale))
+        for call, want in zip((one, few), fresh):
+            got = torch.full_like(want, FILL)
+            call(got, ws)
+            assert torch.equal(got, want)
+
+
+def test_two_calls_at_once_and_a_recorded_one(T):   # noqa: F811
+    gen = torch.Generator(device="cuda").manual_seed(32)
+    m, n = 8192, 1024
+    W, scale = random_ints(gen, m, n), (torch.rand(n, generator=gen, device="cuda") * 0.01).half()
+    sides = []
+    for rows in (20, 70):
+        q, row_scale = make_rows(T, gen, rows, m)
+        ws = torch.zeros(T.teal_workspace_bytes_gemm_w8(rows, m, n), dtype=torch.uint8, device="cuda")
+        sides.append((rows, q, row_scale, torch.empty(rows, n, device="cuda"), ws, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for rows, q, row_scale, y, ws, stream in sides:
+            T.check(T.teal_gemm_w8_ex([W], [scale], [y], [n], q, row_scale, rows, m, ws, stream=stream.cuda_stream, tile_rows=16,
+                                      tile_cols=128, splits=8))
+    torch.cuda.synchronize()
+    for rows, q, row_scale, y, _, _ in sides:
+        assert torch.equal(y, product(q, row_scale, W, scale))
+
+    rows, q, row_scale, y, ws, _ = sides[0]
+    W2, y2 = random_ints(gen, m, 208), torch.empty(rows, 208, device="cuda")
+    ws = torch.zeros(T.teal_workspace_bytes_gemm_w8(rows, m, n + 208), dtype=torch.uint8, device="cuda")
+    run = T.prepare(lambda: T.teal_gemm_w8_multi([W, W2], [scale, scale], [y, y2], [n, 208], q, row_scale, rows, m, ws))
+    for _ in range(3):
+        q[:, :m] = random_ints(gen, rows, m)
+        y.fill_(FILL)
+        y2.fill_(FILL)
+        T.check(run())
+        assert torch.equal(y, product(q, row_scale, W, scale))
+        assert torch.equal(y2, product(q, row_scale, W2, scale[:208]))
