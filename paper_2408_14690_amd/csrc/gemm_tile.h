@@ -112,7 +112,8 @@ struct TileProduct {
     static constexpr int kRowsPerLoad = F::kMx4 ? 2048 / BN : 1024 / kRowBytes;     // rows of W that a load covers
     static constexpr int kRowStep = kRowsPerLoad * kLoadWaves;
     static constexpr int kUnit = F::kBytes == 2 ? 32 : 16;             // bytes that a permutation keeps together
-    static constexpr int kUnitMask = kRowBytes / HALVES / kUnit < 16 ? kRowBytes / HALVES / kUnit - 1 : 15;
+    static constexpr int kHalfUnits = kRowBytes / HALVES / kUnit;      // of one matrix in a row
+    static constexpr int kUnitMask = kRowBytes / kUnit < 16 ? kRowBytes / kUnit - 1 : 15;
     // A lane's permutation in its loads of W repeats with the bits of the row that it depends on.
     static constexpr int kPeriod = F::kBytes == 2 ? 16 : 32;
     static constexpr int kWLanes = F::kMx4 || kRowStep % kPeriod == 0 ? 1 : 2;
@@ -128,12 +129,10 @@ struct TileProduct {
 
     static __device__ __forceinline__ int swizzle(int k)
     {
+        // Rows of 128 bytes have half of the banks each: four of every eight rows that are read together lie in the same half.
+        if (F::kBytes == 1 && kRowBytes == 128) return (k >> 1 & 3) | (k >> 4 & 1) << 2;
         return (F::kBytes == 2 ? (k & 3) | (k >> 3 & 1) << 2 : (k & 7) | (k >> 4 & 1) << 3) & kUnitMask;
     }
-
-    // mx4: a unit's two chunks of 16 bytes change places every four channels, so that the lanes that write one of the two
-    // touch all banks.
-    static __device__ __forceinline__ int flip(int k) { return F::kMx4 ? (k >> 2 & 1) * 16 : 0; }
 
     unsigned lds;                                // of the ring
     int wave, lane, wm, wn;
@@ -148,6 +147,7 @@ struct TileProduct {
     int s_pitch;                                 // bytes between tiles of one block row
     int block_row;
     unsigned scale_at, value_at[4];
+    int other_first;                             // whether it writes the second of a unit's two chunks before the first
 
     __device__ __forceinline__ void begin(void *smem)
     {
@@ -174,10 +174,14 @@ struct TileProduct {
             const int col = min(col0 + 32 * in_half, n - 32);
             scale_at = kSlabX + kCodes + half * (kScales / HALVES) + (block_row / 8) * kMx4TileBytes + block_row % 8 * 16 +
                        col / 32 % 16;
+            // Eight lanes write together.  They have a row of 512 bytes, every second unit of 32: half of them begin with
+            // their units' other chunks, or four would meet four in the same banks.
+            other_first = kRowBytes == 512 ? threadIdx.x >> 2 & 1 : 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                value_at[q] = block_row * kRowBytes + half * (kRowBytes / HALVES) +
-                              ((2 * in_half + q / 2) ^ swizzle(block_row)) * 32 + (q % 2 * 16 ^ flip(block_row));
+                value_at[q] = block_row * kRowBytes +
+                              ((half * kHalfUnits + 2 * in_half + q / 2) ^ swizzle(block_row)) * 32 +
+                              (q ^ other_first) % 2 * 16;
         }
     }
 
@@ -206,15 +210,13 @@ struct TileProduct {
         }
         const int at = chunk * 16;
         w_row = at / kRowBytes;
-        const int half = HALVES == 1 ? 0 : at % kRowBytes / (kRowBytes / 2);
-        const int in_half = at % (kRowBytes / HALVES);
         w_pitch = n * F::kBytes;
 #pragma unroll
         for (int v = 0; v < kWLanes; ++v) {
             const int row = w_row + v * kRowStep;
-            const int unit = in_half / kUnit ^ swizzle(row);
-            const int col = min(col0 + (unit * kUnit + in_half % kUnit) / F::kBytes, n - 16 / F::kBytes);
-            w_lane[v] = w_of(half) + (long long)row * w_pitch + (long long)col * F::kBytes;
+            const int unit = at % kRowBytes / kUnit ^ swizzle(row);
+            const int col = min(col0 + (unit % kHalfUnits * kUnit + at % kUnit) / F::kBytes, n - 16 / F::kBytes);
+            w_lane[v] = w_of(unit / kHalfUnits) + (long long)row * w_pitch + (long long)col * F::kBytes;
         }
     }
     // Which 8 rows of X the wavefront's load j takes: where there are fewer loads than wavefronts some load the same.
@@ -283,11 +285,12 @@ struct TileProduct {
         const unsigned buffer = lds + kRing + to * kSlabW;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+            const unsigned codes = other_first ? b.codes[q ^ 1] : b.codes[q];
             u32x4 v;
-            v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 0));
-            v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 1));
-            v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 2));
-            v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.codes[q], sc, 3));
+            v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 0));
+            v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 1));
+            v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 2));
+            v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 3));
             *(lds_out)(uintptr_t)(buffer + value_at[q]) = v;
         }
     }
@@ -311,18 +314,16 @@ struct TileProduct {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
                     typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
                     const int k = 32 * ks + 8 * g + l / 4;             // and 4 further
-                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 +
-                                      l % 4 * 8;                       // flip(k) is 0
+                    const lds_ptr p = w + k * kRowBytes + ((half * kHalfUnits + piece) ^ swizzle(k)) * 32 + l % 4 * 8;
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
-                    const lds_ptr p4 = w + (k + 4) * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 32 +
-                                       (l % 4 * 8 ^ flip(4));
-                    const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p4));
+                    const uint2 b = __builtin_bit_cast(
+                        uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * kRowBytes)));
                     W[f] = u32x4{a.x, a.y, b.x, b.y};
                 } else {
                     typedef int i32x2 __attribute__((ext_vector_type(2)));
                     typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
                     const int k = 64 * ks + 16 * g + l / 2;            // and 8 further
-                    const lds_ptr p = w + k * kRowBytes + half * (kRowBytes / 2) + (piece ^ swizzle(k)) * 16 + l % 2 * 8;
+                    const lds_ptr p = w + k * kRowBytes + ((half * kHalfUnits + piece) ^ swizzle(k)) * 16 + l % 2 * 8;
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)p));
                     const uint2 b = __builtin_bit_cast(
                         uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(p + 8 * kRowBytes)));
