@@ -134,6 +134,13 @@ struct TileProduct {
         return (F::kBytes == 2 ? (k & 3) | (k >> 3 & 1) << 2 : (k & 7) | (k >> 4 & 1) << 3) & kUnitMask;
     }
 
+    // Place of a unit of channel k in its row.  (Where the permutation stays within a matrix's units, its part is a constant.)
+    static __device__ __forceinline__ int unit_at(int half, int unit, int k)
+    {
+        if (kHalfUnits >= (F::kBytes == 2 ? 8 : 16)) return half * (kRowBytes / HALVES) + (unit ^ swizzle(k)) * kUnit;
+        return ((half * kHalfUnits + unit) ^ swizzle(k)) * kUnit;
+    }
+
     unsigned lds;                                // of the ring
     int wave, lane, wm, wn;
     int load_wave;                               // among those that load
@@ -179,8 +186,7 @@ struct TileProduct {
             other_first = kRowBytes == 512 ? threadIdx.x >> 2 & 1 : 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                value_at[q] = block_row * kRowBytes +
-                              ((half * kHalfUnits + 2 * in_half + q / 2) ^ swizzle(block_row)) * 32 +
+                value_at[q] = block_row * kRowBytes + unit_at(half, 2 * in_half + q / 2, block_row) +
                               (q ^ other_first) % 2 * 16;
         }
     }
@@ -314,7 +320,7 @@ struct TileProduct {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
                     typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
                     const int k = 32 * ks + 8 * g + l / 4;             // and 4 further
-                    const lds_ptr p = w + k * kRowBytes + ((half * kHalfUnits + piece) ^ swizzle(k)) * 32 + l % 4 * 8;
+                    const lds_ptr p = w + k * kRowBytes + unit_at(half, piece, k) + l % 4 * 8;
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
                     const uint2 b = __builtin_bit_cast(
                         uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * kRowBytes)));
@@ -323,7 +329,7 @@ struct TileProduct {
                     typedef int i32x2 __attribute__((ext_vector_type(2)));
                     typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
                     const int k = 64 * ks + 16 * g + l / 2;            // and 8 further
-                    const lds_ptr p = w + k * kRowBytes + ((half * kHalfUnits + piece) ^ swizzle(k)) * 16 + l % 2 * 8;
+                    const lds_ptr p = w + k * kRowBytes + unit_at(half, piece, k) + l % 2 * 8;
                     const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)p));
                     const uint2 b = __builtin_bit_cast(
                         uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(p + 8 * kRowBytes)));

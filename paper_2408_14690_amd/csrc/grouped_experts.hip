@@ -430,8 +430,12 @@ namespace {
 //   2048 tokens (r = 512)                 128 x 128 1313 / 691, 128 x 256 1010 / 603, 256 x 256 1013 / 667
 //   8192 tokens (r = 2048)                128 x 256 3753 / 2040, 256 x 256 3537 / 2043
 //   4096 tokens, 8 of 128 experts of 2048 -> 768 (r = 256)         128 x 128 334 / 308, 128 x 256 264 / 260, 256 x 256 275 / 257
-//   mx4, where every block converts what it reads: r = 4 32 x 128 169 / 90, 64 x 128 slower; r = 64 64 x 128 281 / 181,
-//   128 x 256 315 / 294; r = 512 64 x 128 1472 / 782, 256 x 128 1239 / 672, 256 x 256 1168 / 845
+//   mx4, where every block converts what it reads, 2 of 8 experts of 4096 -> 14336:
+//   r = 4      32 x 128 169 / 90, 64 x 128 slower
+//   r = 64     64 x 128 268 / 177, 256 x 128 295 / 145, 256 x 256 291 / 265
+//   r = 128    64 x 128 426 / 260, 256 x 128 412 / 231, 256 x 256 400 / 346
+//   r = 512    64 x 128 1427 / 754, 256 x 128 1093 / 646, 256 x 256 986 / 751
+//   1200 tokens, 6 of 64 experts of 2048 -> 1408 (r = 112)         64 x 128 162 / 107, 256 x 128 195 / 133, 256 x 256 180 / 130
 struct GroupedShape {
     int bm, bn;
 };
@@ -446,7 +450,7 @@ GroupedShape grouped_shape(const GroupedHostArgs &h, int cols)
         const double tiles = r <= bm / 2 ? experts : experts * (r / bm + 0.5);
         return std::ceil(tiles * ((cols + bn - 1) / bn) / 256) * slab;
     };
-    if (mx4) return {256, time(256, 128, 1.1) < time(256, 256, 1.85) ? 128 : 256};
+    if (mx4) return {256, time(256, 128, 0.96) < time(256, 256, 1.7) ? 128 : 256};
     const double narrow = time(128, 128, 0.65), wide = time(128, 256, 1.0), large = time(256, 256, 1.85);
     if (large < wide && large < narrow) return {256, 256};
     return {128, narrow < wide ? 128 : 256};
@@ -458,7 +462,7 @@ hipError_t run_grouped(const GroupedHostArgs &h, GroupedShape s, hipStream_t str
     if (h.scale[0]) {
         if (s.bm == 32) return Call<WeightsMx4, TileShape<32, 128, 1, 4, 4, 4>>::run(h, stream);
         if (s.bm == 64) return Call<WeightsMx4, TileShape<64, 128, 1, 4, 3, 4>>::run(h, stream);
-        // (with wavefronts that load beside them those of 256 x 256 would have 168 registers each: 1240 us where 1168)
+        // (with wavefronts that load beside them those of 256 x 256 would have 168 registers each, and be 6 % slower)
         return s.bn == 128 ? Call<WeightsMx4, TileShape<256, 128, 4, 1, 3, 4>>::run(h, stream)
                            : Call<WeightsMx4, TileShape<256, 256, 2, 4, 2>>::run(h, stream);
     }
