@@ -385,3 +385,62 @@ def test_a_mixture_of_experts_from_logits_to_its_output(T, fmt):   # noqa: F811
     # x as fp16 (half a step, 2^-11, or 2^-25 where it is tiny) and h as fp16 or bf16 (2^-8): of the sums of sizes
     scale = float(out.abs().max())
     assert float((eager[:few] - out).abs().max()) <= scale * f * (2.0 ** -8 + 2.0 ** -9)
+
+
+def test_offsets_beyond_32_bits_in_the_weights(T):   # noqa: F811
+    """80 experts of 8192 x 4096, more than 2^31 weights each of gate, up and W_down; the last two are chosen."""
+    gen = torch.Generator(device="cuda").manual_seed(51)
+    experts, m, f, tokens, top_k = 80, 8192, 4096, 20, 2
+    gate, up = (torch.empty(experts, m, f, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    down = torch.empty(experts, f, m, dtype=torch.bfloat16, device="cuda")
+    assert gate[:experts - 2].numel() > 2 ** 31
+    for w in (gate, up, down):
+        w[:experts - 2] = float("nan")
+        w[experts - 2:] = torch.randint(-2, 3, w[experts - 2:].shape, generator=gen, device="cuda").bfloat16()
+    idx = torch.tensor([[experts - 2, experts - 1]] * tokens, dtype=torch.int32, device="cuda")
+    order, start = run_arrange(T, idx, experts)
+    x = torch.randint(0, 2, (tokens, m), generator=gen, device="cuda").bfloat16()
+    h = torch.empty(tokens * top_k, f, dtype=torch.bfloat16, device="cuda")
+    T.check(T.teal_grouped_experts_bf16_gate_up(gate, up, experts, order, start, tokens, top_k, x, h, m, f))
+    for i, e in enumerate((experts - 2, experts - 1)):
+        g, u = x.double() @ gate[e].double(), x.double() @ up[e].double()       # whole numbers, exact in fp32
+        want = g * torch.sigmoid(g) * u
+        off = want.abs() * (2.0 ** -8 + 2.0 ** -16) + 1.5e-36 * u.abs() + 2.0 ** -133
+        assert bool(((h[i * tokens:(i + 1) * tokens].double() - want).abs() <= off).all())
+    ones = torch.randint(-1, 2, h.shape, generator=gen, device="cuda").bfloat16()
+    weight, y = torch.ones(tokens, top_k, device="cuda"), torch.empty(tokens, m, device="cuda")
+    ws = torch.zeros(T.teal_workspace_bytes_grouped_experts(tokens * top_k, m), dtype=torch.uint8, device="cuda")
+    T.check(T.teal_grouped_experts_bf16_down(down, experts, order, start, tokens, top_k, idx, weight, ones, y, f, m, ws))
+    want = sum(ones[i * tokens:(i + 1) * tokens].double() @ down[experts - 2 + i].double() for i in range(2))
+    assert torch.equal(y.double(), want)                                            # whole numbers below 2^24
+
+
+def test_offsets_beyond_32_bits_in_the_rows(T):   # noqa: F811
+    """2^20 pairs of 2064 columns: more than 2^31 numbers of H."""
+    gen = torch.Generator(device="cuda").manual_seed(52)
+    experts, m, f, n, tokens, top_k = 4, 8, 2064, 16, 1 << 19, 2
+    gate, up = (torch.randint(-2, 3, (experts, m, f), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    down = torch.randint(-2, 3, (experts, f, n), generator=gen, device="cuda").bfloat16()
+    idx = torch.rand(tokens, experts, generator=gen, device="cuda").argsort(-1)[:, :top_k].int().contiguous()
+    order, start = run_arrange(T, idx, experts)
+    x = torch.randint(-2, 3, (tokens, m), generator=gen, device="cuda").bfloat16()
+    h = torch.full((tokens * top_k, f), FILL, dtype=torch.bfloat16, device="cuda")
+    assert h.numel() > 2 ** 31
+    T.check(T.teal_grouped_experts_bf16_gate_up(gate, up, experts, order, start, tokens, top_k, x, h, m, f))
+    y = torch.full((tokens, n), FILL, device="cuda")
+    weight = torch.rand(tokens, top_k, generator=gen, device="cuda")
+    ws = torch.zeros(T.teal_workspace_bytes_grouped_experts(tokens * top_k, n), dtype=torch.uint8, device="cuda")
+    T.check(T.teal_grouped_experts_bf16_down(down, experts, order, start, tokens, top_k, idx, weight, h, y, f, n, ws))
+    place = torch.empty(tokens * top_k, dtype=torch.long, device="cuda")
+    place[order.long()] = torch.arange(tokens * top_k, device="cuda")
+    for b in (0, 1, 12345, tokens // 2, tokens - 2, tokens - 1):
+        total, off = 0, 0
+        for j in range(top_k):
+            e, at = int(idx[b, j]), int(place[b * top_k + j])
+            g, u = (x[b].double() @ w[e].double() for w in (gate, up))
+            want = g * torch.sigmoid(g) * u
+            row = h[at].double()
+            assert bool(((row - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -16) + 2.0 ** -133).all())
+            total = total + float(weight[b, j]) * (row @ down[e].double())
+            off = off + float(weight[b, j]) * (row.abs() @ down[e].double().abs())
+        assert bool(((y[b].double() - total).abs() <= off * (f * 2.0 ** -23 + (top_k + 1) * 2.0 ** -24)).all())

@@ -368,3 +368,27 @@ def test_two_calls_at_once_and_a_recorded_one(T):   # noqa: F811
         T.check(run())
         assert torch.equal(y, product(q, row_scale, W, scale))
         assert torch.equal(y2, product(q, row_scale, W2, scale[:208]))
+
+
+def test_offsets_beyond_32_bits(T):   # noqa: F811
+    """2^20 rows of 2064: more than 2^31 numbers of X, Q and Y."""
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    rows, m, n = T.TEAL_MAX_ROWS, 2064, 2064
+    x = torch.empty(rows, m, dtype=torch.float16, device="cuda").normal_(generator=gen)
+    pitch = T.teal_quantized_pitch(m)
+    q, row_scale = torch.empty(rows, pitch, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    T.check(T.teal_quantize_rows(x, T.TEAL_F16, rows, m, 0.25, q, row_scale))
+    assert x.numel() > 2 ** 31 and q.numel() > 2 ** 31
+    for at in (0, rows // 2 - 3, rows - 40):
+        want_q, want_scale = quantized(x[at:at + 40].double().cpu().numpy(), 0.25)
+        assert np.array_equal(q[at:at + 40, :m].cpu().numpy(), want_q)
+        assert np.array_equal(row_scale[at:at + 40].cpu().numpy(), want_scale)
+    del x
+    W, scale = random_ints(gen, m, n), (torch.rand(n, generator=gen, device="cuda") * 0.01).half()
+    y = torch.full((rows, n), float("nan"), device="cuda")
+    ws = torch.zeros(T.teal_workspace_bytes_gemm_w8(rows, m, n), dtype=torch.uint8, device="cuda")
+    T.check(T.teal_gemm_w8(W, scale, q, row_scale, rows, y, m, n, ws))
+    assert not bool(torch.isnan(y).any())
+    for at in range(0, rows, rows // 16):
+        part = slice(at + rows // 16 - 1000, at + rows // 16)
+        assert torch.equal(y[part], product(q[part], row_scale[part], W, scale))
