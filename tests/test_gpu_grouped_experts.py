@@ -9,6 +9,7 @@ are not off at all."""
 import numpy as np
 import pytest
 
+import teal_inputs as ti
 from test_gpu_many_rows import FILL
 from test_gpu_mx4 import T  # noqa: F401
 
@@ -385,6 +386,34 @@ def test_a_mixture_of_experts_from_logits_to_its_output(T, fmt):   # noqa: F811
     # x as fp16 (half a step, 2^-11, or 2^-25 where it is tiny) and h as fp16 or bf16 (2^-8): of the sums of sizes
     scale = float(out.abs().max())
     assert float((eager[:few] - out).abs().max()) <= scale * f * (2.0 ** -8 + 2.0 ** -9)
+
+
+@pytest.mark.parametrize("tokens", [4, 60, 700])
+def test_a_block_of_nan_weights_stays_in_its_columns(T, tokens):   # noqa: F811
+    """The scale byte 255 makes a block of 32 outputs NaN, whatever its codes, for the rows of its expert."""
+    c = Case(T, "mx4", tokens, 2, 3, 136, 320, 288)
+    clean_h = c.run_gate_up()
+    clean_y = c.run_down(clean_h)
+    assert bool(torch.isfinite(clean_y).all())
+    places = torch.from_numpy(np.asarray(ti.mx4_scale_places(c.m, c.f))).long()
+    for weights in (c.gate, c.up):
+        kept = weights[1].clone()
+        weights[1][1, int(places[c.m - 1, 4])] = 255
+        weights[0][1, c.m - 1, 4 * 16:5 * 16] = 0                  # codes of zeros: NaN none the less
+        h = c.run_gate_up()
+        bad = torch.zeros_like(h, dtype=torch.bool)
+        a, b = int(c.start[1]), int(c.start[2])
+        bad[a:b, 4 * 32:5 * 32] = True
+        assert torch.equal(torch.isnan(h), bad) and torch.equal(h[~bad], clean_h[~bad])
+        weights[1].copy_(kept)
+        clean_h = c.run_gate_up()                                  # (those codes are zeros now)
+    clean_y = c.run_down(clean_h)
+    places = torch.from_numpy(np.asarray(ti.mx4_scale_places(c.f, c.n))).long()
+    c.down[1][2, int(places[0, 8])] = 255
+    y = c.run_down(clean_h)
+    bad = torch.zeros_like(y, dtype=torch.bool)
+    bad[(c.idx == 2).any(1), 8 * 32:] = True
+    assert torch.equal(torch.isnan(y), bad) and torch.equal(y[~bad], clean_y[~bad])
 
 
 def test_offsets_beyond_32_bits_in_the_weights(T):   # noqa: F811
