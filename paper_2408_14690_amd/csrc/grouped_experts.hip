@@ -426,10 +426,10 @@ namespace {
 // they fill the units; compared by the rounds of tiles that the units take and the time of a slab (us, measured on
 // full launches), the last tile of an expert taken as half empty.  What was measured (us, gate and up / down):
 //   bf16, 64 tokens, 2 of 8 experts of 4096 -> 14336 (r = 16)      32 x 128 347 / 185, 64 x 128 348 / 160, 128 x 256 346 / 179
-//   256 tokens of the same (r = 64)       64 x 128 447 / 239, 128 x 128 415 / 185, 128 x 256 380 / 213, 256 x 256 416 / 289
-//   2048 tokens (r = 512)                 128 x 128 1313 / 691, 128 x 256 1010 / 603, 256 x 256 1013 / 667
+//   256 tokens of the same (r = 64)       64 x 128 444 / 241, 128 x 128 411 / 185, 128 x 256 380 / 214, 256 x 256 413 / 290
+//   2048 tokens (r = 512)                 128 x 128 1302 / 695, 128 x 256 998 / 603, 256 x 256 1027 / 744
 //   8192 tokens (r = 2048)                128 x 256 3753 / 2040, 256 x 256 3537 / 2043
-//   4096 tokens, 8 of 128 experts of 2048 -> 768 (r = 256)         128 x 128 334 / 308, 128 x 256 264 / 260, 256 x 256 275 / 257
+//   4096 tokens, 8 of 128 experts of 2048 -> 768 (r = 256)         128 x 128 335 / 314, 128 x 256 262 / 260, 256 x 256 276 / 265
 //   mx4, where every block converts what it reads, 2 of 8 experts of 4096 -> 14336:
 //   r = 4      32 x 128 169 / 90, 64 x 128 slower
 //   r = 64     64 x 128 268 / 177, 256 x 128 295 / 145, 256 x 256 291 / 265
