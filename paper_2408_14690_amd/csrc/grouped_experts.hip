@@ -1,9 +1,8 @@
 // A mixture of experts for many tokens: the pairs of a token and an expert that a router chose, sorted by expert, and the
 // products of every expert with the rows that are its own.
 #include "gemm_tile.h"
+#include "grouped_shape.h"
 #include "teal_internal.h"
-
-#include <cmath>
 
 namespace teal {
 
@@ -421,39 +420,9 @@ hipError_t launch_arrange_experts(const int *idx, int tokens, int top_k, int exp
 
 namespace {
 
-// Shape of the tiles, by the rows that an expert has on average (r).  Few rows: what counts is that W is read once and much
-// of it at a time, two blocks on a compute unit.  Many: the tiles that load least for what they multiply, as long as
-// they fill the units; compared by the rounds of tiles that the units take and the time of a slab (us, measured on
-// full launches), the last tile of an expert taken as half empty.  What was measured (us, gate and up / down):
-//   bf16, 64 tokens, 2 of 8 experts of 4096 -> 14336 (r = 16)      32 x 128 347 / 185, 64 x 128 348 / 160, 128 x 256 346 / 179
-//   256 tokens of the same (r = 64)       64 x 128 444 / 241, 128 x 128 411 / 185, 128 x 256 380 / 214, 256 x 256 413 / 290
-//   2048 tokens (r = 512)                 128 x 128 1302 / 695, 128 x 256 998 / 603, 256 x 256 1027 / 744
-//   8192 tokens (r = 2048)                128 x 256 3753 / 2040, 256 x 256 3537 / 2043
-//   4096 tokens, 8 of 128 experts of 2048 -> 768 (r = 256)         128 x 128 335 / 314, 128 x 256 262 / 260, 256 x 256 276 / 265
-//   mx4, where every block converts what it reads, 2 of 8 experts of 4096 -> 14336:
-//   r = 4      32 x 128 169 / 90, 64 x 128 slower
-//   r = 64     64 x 128 268 / 177, 256 x 128 295 / 145, 256 x 256 291 / 265
-//   r = 128    64 x 128 426 / 260, 256 x 128 412 / 231, 256 x 256 400 / 346
-//   r = 512    64 x 128 1427 / 754, 256 x 128 1093 / 646, 256 x 256 986 / 751
-//   1200 tokens, 6 of 64 experts of 2048 -> 1408 (r = 112)         64 x 128 162 / 107, 256 x 128 195 / 133, 256 x 256 180 / 130
-struct GroupedShape {
-    int bm, bn;
-};
-GroupedShape grouped_shape(const GroupedHostArgs &h, int cols)
+GroupedShape shape_of(const GroupedHostArgs &h, int cols)
 {
-    const bool mx4 = h.scale[0] != nullptr;
-    const long long pairs = (long long)h.tokens * h.top_k;
-    const double experts = pairs < h.experts ? (double)pairs : (double)h.experts, r = pairs / experts;
-    if (r <= 8) return {32, 128};
-    if (r <= (mx4 ? 128 : 32)) return {64, 128};
-    auto time = [&](int bm, int bn, double slab) {
-        const double tiles = r <= bm / 2 ? experts : experts * (r / bm + 0.5);
-        return std::ceil(tiles * ((cols + bn - 1) / bn) / 256) * slab;
-    };
-    if (mx4) return {256, time(256, 128, 0.96) < time(256, 256, 1.7) ? 128 : 256};
-    const double narrow = time(128, 128, 0.65), wide = time(128, 256, 1.0), large = time(256, 256, 1.85);
-    if (large < wide && large < narrow) return {256, 256};
-    return {128, narrow < wide ? 128 : 256};
+    return grouped_shape(h.scale[0] != nullptr, (long long)h.tokens * h.top_k, h.experts, cols);
 }
 
 template <template <class, class> class Call>
@@ -477,12 +446,12 @@ hipError_t run_grouped(const GroupedHostArgs &h, GroupedShape s, hipStream_t str
 
 hipError_t launch_grouped_gate_up(const GroupedHostArgs &h, hipStream_t stream)
 {
-    return run_grouped<GateUp>(h, grouped_shape(h, 2 * h.n), stream);
+    return run_grouped<GateUp>(h, shape_of(h, 2 * h.n), stream);
 }
 
 hipError_t launch_grouped_down(const GroupedHostArgs &h, hipStream_t stream)
 {
-    return run_grouped<Down>(h, grouped_shape(h, h.n), stream);
+    return run_grouped<Down>(h, shape_of(h, h.n), stream);
 }
 
 }  // namespace teal
