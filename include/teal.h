@@ -637,6 +637,8 @@ teal_status teal_gemm_w8_ex(int count, const int8_t *const *Wq, const void *cons
  * of order that has an expert e; x is the row of X of pair order[i]'s token.  Products are exact and summed in fp32;
  * SiLU(g) * u is off by less than 2^-16 of itself before its rounding to bf16 (for g below -87, where it is smaller
  * than 1.5 10^-36 |u|, it may be 0; a g of -infinity gives NaN).  Rows of H from start[experts] on are left as they are.
+ * Weights, X and H count as what they are, subnormal numbers too; a microscaled weight beyond the range of bf16 (scale bytes
+ * 253 and 254) as the infinity that teal_unpack_mx4 gives, in its own column.
  *   Wt_gate, Wt_up [experts][m][f] bf16; Wq_* [experts][m][f/2], scale_* [experts] times teal_mx4_scale_bytes(m, f)
  *          bytes, all 16-byte aligned, as for teal_sparse_experts_*.
  *   X_bf16 [tokens][m] bf16 (the weights' type: a matrix instruction has one), H_bf16 [tokens * top_k][f] bf16, both
