@@ -40,8 +40,15 @@
  *     teal_workspace_bytes(m, n) bytes, 256-byte aligned.  It must be
  *     zero-filled once before its first use (hipMemset, torch.zeros); every
  *     call that returns TEAL_OK leaves it ready for the next call, of any
- *     shape that fits.  Its contents are otherwise the library's (the one
- *     part a caller may read is described under teal_survivors_offset).
+ *     shape that fits.  A call writes to as many of its bytes as it asks for
+ *     and leaves sums there behind the first 1 MB, which matters to two
+ *     kinds: teal_sparse_gemv_*_stack and teal_sparse_mlp_* have further
+ *     counters behind their first region (the workspace of the first group;
+ *     teal_mlp_down_region_offset bytes).  A workspace is ready for them if
+ *     each call since it was zero-filled asked for no more than that region,
+ *     or was of the same kind and dimensions.  Its contents are otherwise the
+ *     library's (the one part a caller may read is described under
+ *     teal_survivors_offset).
  *     Calls that may run concurrently need distinct workspaces.
  *   - No global state; any host thread may call with any current device, as
  *     long as the pointers belong to it.
@@ -87,7 +94,8 @@ size_t teal_workspace_bytes(int m, int n);
  * with one matrix) as an int32 at byte offset teal_survivors_offset() + 4 * k
  * of its workspace; realised sparsity = 1 - count / m.  The values are
  * complete when the call has completed on its stream and stay until the next
- * call on that workspace; the caller reads them as it reads any device memory.
+ * call on that workspace (of whatever kind: calls that state no count leave
+ * sums there); the caller reads them as it reads any device memory.
  * They cost no extra launch and no extra pass over x: the thread blocks of a
  * matrix's first output tile report the counts of their slices, and the block
  * that finishes that tile adds them.
@@ -217,7 +225,8 @@ teal_status teal_sparse_gemv_bf16_multi_pitch(int count, const void *const *Wt_b
  *   x_f16, m  HOST arrays [groups]: device pointer to each group's input and
  *           its length.
  *   workspace  at least teal_workspace_bytes_stack(groups, counts, n, m), zero
- *           before first use like every workspace.  The groups' regions follow
+ *           before first use like every workspace (and since then used by
+ *           what the conventions allow).  The groups' regions follow
  *           each other; region g is laid out and sized like the workspace of
  *           group g's own call (teal_workspace_bytes(m_g, sum of its n)), so
  *           its survivor report sits teal_survivors_offset() bytes into it.
@@ -566,9 +575,9 @@ teal_status teal_sparse_experts_mx4_swiglu(const uint8_t *Wq, const uint8_t *sca
  * is a hidden state of its own.  Dense but for the threshold of teal_quantize_rows: what many rows keep together is
  * every channel, so nothing is left to skip (Section 5.4.3 discusses a prompt's first half for its accuracy).
  *
- * The calls of this part and the next leave sums and counts in their workspaces.  One may serve them and the calls whose
- * workspace is teal_workspace_bytes or those of a batch or of experts in turn; a workspace of groups (_stack) or of a
- * whole MLP, whose counters lie further on, keeps to its own calls.
+ * The calls of this part and the next leave sums and counts in their workspaces, none of them counts of survivors.  One may
+ * serve them and the calls whose workspace is teal_workspace_bytes or those of a batch or of experts in turn; for one of
+ * groups (_stack) or of a whole MLP see the conventions.
  *
  * 8-bit weights (Section 5.3), W[j][i] = Wq[i][j] * scale[j] as for teal_sparse_gemv_w8: rows to 8-bit integers with a
  * scale each, and products of integers.
@@ -699,7 +708,8 @@ teal_status teal_grouped_experts_mx4_down(const uint8_t *Wq_down, const uint8_t 
  *   1 <= m <= 2^24, 8 <= f <= 2^23, 8 <= d <= 2^24, f % 8 == 0, d % 8 == 0
  *   (16 for int8, 32 for int4 weights).
  *   workspace  at least teal_workspace_bytes_mlp(m, f, d) bytes, zero before
- *           first use like every workspace: the workspace of the gate + up
+ *           first use like every workspace (and since then used by what the
+ *           conventions allow): the workspace of the gate + up
  *           call (survivor counts of gate and up at teal_survivors_offset()),
  *           that of the W_down call at byte teal_mlp_down_region_offset(m, f)
  *           (its survivor count teal_survivors_offset() bytes further), then
