@@ -1137,6 +1137,17 @@ def _row_floats(a, count, what):
     return _typed(a, 4, count, what, "32-bit floats")
 
 
+def _bytes(a, count, what):
+    """8-bit integers, microscaled codes or their scales."""
+    return _typed(a, 1, count, what, "single bytes")
+
+
+def _column_scales(a, count):
+    if _dtype_name(a) == "torch.bfloat16":
+        raise ValueError("scale: fp16 numbers")
+    return _typed(a, 2, count, "scale", "fp16 numbers")
+
+
 _dtype_names = {}
 
 
@@ -1154,14 +1165,14 @@ def teal_quantize_rows(X, type, rows, m, t, Q, row_scale, stream=None) -> int:
     return _call(
         "teal_quantize_rows",
         _typed(X, 2, rows * m, "X", "16-bit floats"), int(type), int(rows), int(m), float(t),
-        _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
+        _bytes(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
 
 
 def teal_quantize_rows_swiglu(gate, up, rows, m, t, Q, row_scale, stream=None) -> int:
     return _call(
         "teal_quantize_rows_swiglu",
         _row_floats(gate, rows * m, "gate"), _row_floats(up, rows * m, "up"), int(rows), int(m), float(t),
-        _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
+        _bytes(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"), _stream(stream))
 
 
 def teal_workspace_bytes_gemm_w8(rows: int, m: int, n: int) -> int:
@@ -1171,7 +1182,7 @@ def teal_workspace_bytes_gemm_w8(rows: int, m: int, n: int) -> int:
 def teal_gemm_w8(Wq, scale_f16, Q, row_scale, rows, Y, m, n, workspace, workspace_bytes=None, stream=None) -> int:
     return _call(
         "teal_gemm_w8",
-        _ptr(Wq, m * n, "Wq"), _ptr(scale_f16, 2 * n, "scale"), _ptr(Q, rows * _pitch_need(m), "Q"),
+        _bytes(Wq, m * n, "Wq"), _column_scales(scale_f16, n), _bytes(Q, rows * _pitch_need(m), "Q"),
         _row_floats(row_scale, rows, "row_scale"), int(rows), _row_floats(Y, rows * n, "Y"), int(m), int(n),
         _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
@@ -1180,10 +1191,10 @@ def _gemm_w8_arguments(Wq_list, scale_list, Y_list, n_list, Q, row_scale, rows, 
     count = len(Wq_list)
     if not (len(scale_list) == len(Y_list) == len(n_list) == count):
         raise ValueError("per-matrix lists must have the same length")
-    W = _pointers([_ptr(w, m * n, "Wq") or 0 for w, n in zip(Wq_list, n_list)])
-    S = _pointers([_ptr(sc, 2 * n, "scale") or 0 for sc, n in zip(scale_list, n_list)])
+    W = _pointers([_bytes(w, m * n, "Wq") or 0 for w, n in zip(Wq_list, n_list)])
+    S = _pointers([_column_scales(sc, n) or 0 for sc, n in zip(scale_list, n_list)])
     Y = _pointers([_row_floats(y, rows * n, "Y") or 0 for y, n in zip(Y_list, n_list)])
-    return (count, W, S, Y, _ints(n_list), _ptr(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"),
+    return (count, W, S, Y, _ints(n_list), _bytes(Q, rows * _pitch_need(m), "Q"), _row_floats(row_scale, rows, "row_scale"),
             int(rows), int(m), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -1218,7 +1229,7 @@ def teal_arrange_experts(idx, tokens, top_k, experts, order, start, workspace, w
         _numbers(start, experts + 1, "start"), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
-def _bf16_rows(a, count, what):
+def _bf16(a, count, what):
     if _dtype_name(a) == "torch.float16":
         raise ValueError(f"{what}: bf16 numbers")
     return _typed(a, 2, count, what, "bf16 numbers")
@@ -1227,12 +1238,12 @@ def _bf16_rows(a, count, what):
 def teal_grouped_experts_bf16_gate_up(Wt_gate, Wt_up, experts, order, start, tokens, top_k, X_bf16, H_bf16, m, f,
                                       stream=None) -> int:
     """H: a row per place of `order`, of the experts' width f."""
-    pairs, need = tokens * top_k, 2 * experts * m * f
+    pairs, need = tokens * top_k, experts * m * f
     return _call(
         "teal_grouped_experts_bf16_gate_up",
-        _ptr(Wt_gate, need, "Wt_gate"), _ptr(Wt_up, need, "Wt_up"), int(experts), _numbers(order, pairs, "order"),
-        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16_rows(X_bf16, tokens * m, "X"),
-        _bf16_rows(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
+        _bf16(Wt_gate, need, "Wt_gate"), _bf16(Wt_up, need, "Wt_up"), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16(X_bf16, tokens * m, "X"),
+        _bf16(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
 
 
 def teal_grouped_experts_mx4_gate_up(Wq_gate, scale_gate, Wq_up, scale_up, experts, order, start, tokens, top_k, X_bf16,
@@ -1240,10 +1251,10 @@ def teal_grouped_experts_mx4_gate_up(Wq_gate, scale_gate, Wq_up, scale_up, exper
     pairs, codes, scales = tokens * top_k, experts * (m * f // 2), experts * _mx4_scale_need(m, f)
     return _call(
         "teal_grouped_experts_mx4_gate_up",
-        _ptr(Wq_gate, codes, "Wq_gate"), _ptr(scale_gate, scales, "scale_gate"), _ptr(Wq_up, codes, "Wq_up"),
-        _ptr(scale_up, scales, "scale_up"), int(experts), _numbers(order, pairs, "order"),
-        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16_rows(X_bf16, tokens * m, "X"),
-        _bf16_rows(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
+        _bytes(Wq_gate, codes, "Wq_gate"), _bytes(scale_gate, scales, "scale_gate"), _bytes(Wq_up, codes, "Wq_up"),
+        _bytes(scale_up, scales, "scale_up"), int(experts), _numbers(order, pairs, "order"),
+        _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _bf16(X_bf16, tokens * m, "X"),
+        _bf16(H_bf16, pairs * f, "H"), int(m), int(f), _stream(stream))
 
 
 def teal_workspace_bytes_grouped_experts(pairs: int, n: int) -> int:
@@ -1255,9 +1266,9 @@ def teal_grouped_experts_bf16_down(Wt_down, experts, order, start, tokens, top_k
     pairs = tokens * top_k
     return _call(
         "teal_grouped_experts_bf16_down",
-        _ptr(Wt_down, 2 * experts * m * n, "Wt_down"), int(experts), _numbers(order, pairs, "order"),
+        _bf16(Wt_down, experts * m * n, "Wt_down"), int(experts), _numbers(order, pairs, "order"),
         _numbers(start, experts + 1, "start"), int(tokens), int(top_k), _numbers(idx, pairs, "idx"),
-        _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"), _row_floats(y, tokens * n, "y"),
+        _row_floats(weight, pairs, "weight"), _bf16(H_bf16, pairs * m, "H"), _row_floats(y, tokens * n, "y"),
         int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -1266,8 +1277,8 @@ def teal_grouped_experts_mx4_down(Wq_down, scale_down, experts, order, start, to
     pairs = tokens * top_k
     return _call(
         "teal_grouped_experts_mx4_down",
-        _ptr(Wq_down, experts * (m * n // 2), "Wq_down"), _ptr(scale_down, experts * _mx4_scale_need(m, n), "scale_down"),
+        _bytes(Wq_down, experts * (m * n // 2), "Wq_down"), _bytes(scale_down, experts * _mx4_scale_need(m, n), "scale_down"),
         int(experts), _numbers(order, pairs, "order"), _numbers(start, experts + 1, "start"), int(tokens), int(top_k),
-        _numbers(idx, pairs, "idx"), _row_floats(weight, pairs, "weight"), _bf16_rows(H_bf16, pairs * m, "H"),
+        _numbers(idx, pairs, "idx"), _row_floats(weight, pairs, "weight"), _bf16(H_bf16, pairs * m, "H"),
         _row_floats(y, tokens * n, "y"), int(m), int(n), _ptr(workspace), _nbytes(workspace, workspace_bytes),
         _stream(stream))

@@ -40,3 +40,36 @@ def test_experts_refuse_64_bit_floats(fmt, down, name):
         else:
             call = T.teal_sparse_experts_mx4 if fmt == "mx4" else T.teal_sparse_experts_bf16
             call(*[[w] for w in weights], [a["t"]], [Y], [64], 8, I, 2, 2, X, 64, WS, BIG, stream=0)
+
+
+def test_weights_and_integers_of_many_rows_have_their_own_types():
+    """Tensors that are large enough, and whose numbers are not those that the call reads."""
+    torch = pytest.importorskip("torch")
+    q, w, sc = torch.zeros(3, 128, dtype=torch.int8), torch.zeros(40, 16, dtype=torch.int8), torch.zeros(16).half()
+    for bad in (dict(q=q.int()), dict(q=q.half()), dict(w=w.int()), dict(w=w.bfloat16()), dict(sc=sc.bfloat16()), dict(sc=sc.float())):
+        a = {**dict(q=q, w=w, sc=sc), **bad}
+        with pytest.raises(ValueError):
+            T.teal_gemm_w8(a["w"], a["sc"], a["q"], U, 3, Y, 40, 16, WS, BIG, stream=0)
+        with pytest.raises(ValueError):
+            T.teal_gemm_w8_multi([a["w"]], [a["sc"]], [Y], [16], a["q"], U, 3, 40, WS, BIG, stream=0)
+        with pytest.raises(ValueError):
+            T.teal_gemm_w8_ex([a["w"]], [a["sc"]], [Y], [16], a["q"], U, 3, 40, WS, BIG, stream=0, tile_rows=16, tile_cols=128)
+    with pytest.raises(ValueError):
+        T.teal_quantize_rows(X, T.TEAL_F16, 3, 40, 0.0, q.int(), U, stream=0)
+    with pytest.raises(ValueError):
+        T.teal_quantize_rows_swiglu(U, U, 3, 40, 0.0, q.half(), U, stream=0)
+    group = (4, I, I, 4, 2)
+    wide, codes = torch.zeros(4, 64, 64).bfloat16(), torch.zeros(4, 64, 32, dtype=torch.uint8)
+    scales = torch.zeros(4, T.teal_mx4_scale_bytes(64, 64), dtype=torch.uint8)
+    for bad in (wide.half(), wide.float()):
+        for pair in ((bad, wide), (wide, bad)):
+            with pytest.raises(ValueError):
+                T.teal_grouped_experts_bf16_gate_up(*pair, *group, X, Y, 64, 64, stream=0)
+        with pytest.raises(ValueError):
+            T.teal_grouped_experts_bf16_down(bad, *group, I, U, X, Y, 64, 64, WS, BIG, stream=0)
+    for bad in ((codes.int(), scales), (codes, scales.int()), (codes.half(), scales)):
+        for four in ((*bad, codes, scales), (codes, scales, *bad)):
+            with pytest.raises(ValueError):
+                T.teal_grouped_experts_mx4_gate_up(*four, *group, X, Y, 64, 64, stream=0)
+        with pytest.raises(ValueError):
+            T.teal_grouped_experts_mx4_down(*bad, *group, I, U, X, Y, 64, 64, WS, BIG, stream=0)
