@@ -238,9 +238,10 @@ __device__ __forceinline__ size_t expert_bytes(int m, int n)
 }
 
 // SiLU(g) * u for a result of 8 bits, by the hardware's exponential and reciprocal: g / (1 + 2^(-g log2 e)) * u.  The product
-// -g log2 e is off by 2^-24 of itself, so for g >= -87 the power by 2^-17.5; the rest adds five steps of 2^-23.  Below that
-// the reciprocal is no normal number (e^-87.3 is 2^-126) and the result may be zero.  (A tile of 256 x 256 has 64 values a
-// thread: 9 us of 66 with a polynomial and a correctly rounded division.)
+// -g log2 e is off by 2^-24 of itself and its constant by 2^-26.1, so for g >= -87 the power by 87 (2^-24 + 2^-26.1) < 2^-17.2;
+// the rest adds five steps of 2^-23: less than 2^-16 together.  Below that the reciprocal is no normal number (e^-87.3 is
+// 2^-126) and the result may be zero.  (A tile of 256 x 256 has 64 values a thread: 9 us of 66 with a polynomial and a
+// correctly rounded division.)
 __device__ __forceinline__ float swiglu_fast(float g, float u)
 {
     return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;

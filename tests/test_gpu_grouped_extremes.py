@@ -92,3 +92,29 @@ def test_every_bf16_number(T, experts):   # noqa: F811
         # each row has 64 numbers, and each column takes one of them
         part = part.reshape(ROWS, 64).contiguous()
         assert torch.equal(down(T, "bf16", (one,), experts, part, 64), part.float())
+
+
+@pytest.mark.parametrize("up", [1.0, -1.3671875, 2.0 ** -20, 3.0 * 2.0 ** 60])
+@pytest.mark.parametrize("experts", [64, 1])
+def test_silu_of_every_bf16_number(T, experts, up):   # noqa: F811
+    """H lies between the roundings of what is 2^-16 smaller and larger, by 2^-148 where that is subnormal; nothing below g = -87
+    is larger than it may be; NaN and infinities come out as the formula in 32 bits has them."""
+    every = dev(np.arange(1 << 16, dtype=np.uint32).astype(np.uint16)).view(torch.bfloat16)
+    f = every.numel()
+    gate, other = (torch.zeros(experts, 8, f, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    gate[:, 3], other[:, 3] = every, up
+    rows = 128
+    x = torch.zeros(rows, 8, dtype=torch.bfloat16, device="cuda")
+    x[:, 3] = 1
+    order = torch.arange(rows, dtype=torch.int32, device="cuda")
+    start = (torch.arange(experts + 1, device="cuda") * (rows // experts)).int()
+    h = torch.empty(rows, f, dtype=torch.bfloat16, device="cuda")
+    T.check(T.teal_grouped_experts_bf16_gate_up(gate, other, experts, order, start, rows, 1, x, h, 8, f))
+    assert bool((h.view(torch.int16) == h[0].view(torch.int16)).all())
+    h, g = h[0], every.double()
+    want = g / (1 + torch.exp(-g)) * up
+    room = want.abs() * 2.0 ** -16 + 2.0 ** -148
+    low, high = ((want + s * room).float().bfloat16() for s in (-1, 1))
+    ok = (h >= low) & (h <= high) | torch.isnan(want) & torch.isnan(h) | torch.isinf(want) & (h.double() == want)
+    ok |= (g < -87) & (h.double().abs() <= 1.5e-36 * abs(up))
+    assert bool(ok.all()), every[~ok][:8].tolist()
