@@ -16,8 +16,9 @@
 // permutation is in the lanes' global addresses, within one row's bytes.
 //
 // What bounds it.  Tiles up to 256 x 128: the way from the L2 caches into LDS, which gives all compute units together about
-// 12 TB/s whatever the tile (int8, 700 rows of 11008 -> 4096: 43 us; with every wavefront loading its part 55, since the
-// address arithmetic and the waits of the loads then stand between its matrix instructions).  256 x 256 loads least for what
+// 12 TB/s whatever the tile (int8, 700 rows of 11008 -> 4096, the weights in the last cache: 43 us; with every wavefront
+// loading its part 55, since the address arithmetic and the waits of the loads then stand between its matrix instructions;
+// 59 with weights from memory).  256 x 256 loads least for what
 // it multiplies (9 TB/s) and has the matrix cores busy; there their rate, which falls with the power that the operands'
 // bits take (7 to 20 % between zeros and random numbers), bounds it with the LDS reads: 4096 x 8192 -> 28672 int8 at
 // 2.3 POPS.  Tiles of few rows: memory, once for W.

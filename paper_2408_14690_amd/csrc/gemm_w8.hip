@@ -399,6 +399,8 @@ hipError_t launch_gemm_w8(const GemmW8HostArgs &h, const GemmShape &sh, hipStrea
     case 64: return launch<TileShape<64, 128, 1, 4, 3, 4>>(a, stream);
     case 128: return launch<TileShape<128, 128, 2, 4, 4, 4>>(a, stream);
     default:
+        // (256 x 256: 168 registers a lane, and 13 more that are stored before the loop over the slabs and read behind it,
+        // once a tile; nothing is spilled in the loop)
         return sh.bn == 128 ? launch<TileShape<256, 128, 4, 2, 3, 4>>(a, stream)
                             : launch<TileShape<256, 256, 2, 4, 2, 4>>(a, stream);
     }
